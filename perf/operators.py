@@ -68,7 +68,9 @@ def draw(rng):
     page = rng.choice((32, 64, 128))
     width = kv_heads * d_head
     length = _log_int(rng, 1, 65536)
-    users = _log_int(rng, 1, max(1, min(256, 400_000_000 // (length * width))))
+    most = 400_000_000 if kind in ("attend", "window") else 60_000_000      # features held
+    length = min(length, most // width)
+    users = _log_int(rng, 1, max(1, min(256, most // (length * width))))
     case = _case("", kind, dtype, users, length, kv_heads, kv_heads * group, d_head, page, ragged=rng.random() < 0.6)
     del case["name"]
     if kind in ("attend", "window"):
