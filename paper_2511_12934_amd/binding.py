@@ -170,6 +170,7 @@ def load():
     lib.aif_user_profile_begin.argtypes = [vp, C.c_int32]
     lib.aif_user_profile_end.restype = C.c_int
     lib.aif_user_profile_end.argtypes = [vp, C.POINTER(C.c_double), C.POINTER(C.c_int32)]
+    _declare_cache(lib)
     _lib = lib
     return lib
 
@@ -483,6 +484,272 @@ class UserContext:
     def close(self):
         if self._h:
             self._lib.aif_user_destroy(self._h)
+            self._h = C.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+# ---- the user cache (include/aif_cache.h) ---------------------------------------------------------------------------
+class aif_cache_config(C.Structure):
+    _fields_ = [("dtype", C.c_int), ("n_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32),
+                ("scale", C.c_float), ("page_len", C.c_int32), ("n_pages", C.c_int32), ("max_seqs", C.c_int32),
+                ("max_len", C.c_int32), ("max_requests", C.c_int32), ("max_queries", C.c_int32)]
+
+
+class aif_cache_append_req(C.Structure):
+    _fields_ = [("seq", C.c_int32), ("n_rows", C.c_int32), ("keys", C.c_void_p), ("vals", C.c_void_p),
+                ("key_stride", C.c_int64), ("val_stride", C.c_int64)]
+
+
+class aif_cache_attend_req(C.Structure):
+    _fields_ = [("seq", C.c_int32), ("n_q", C.c_int32), ("q", C.c_void_p), ("out", C.c_void_p), ("lse_out", C.c_void_p),
+                ("positions", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64), ("sinks", C.c_int32),
+                ("window", C.c_int32)]
+
+
+class aif_cache_read_req(C.Structure):
+    _fields_ = [("seq", C.c_int32), ("first", C.c_int32), ("n_rows", C.c_int32), ("reserved", C.c_int32),
+                ("keys_out", C.c_void_p), ("vals_out", C.c_void_p), ("key_stride", C.c_int64), ("val_stride", C.c_int64)]
+
+
+CACHE_EXPORTS = ("aif_cache_page_bytes", "aif_cache_init", "aif_cache_destroy", "aif_cache_last_error", "aif_cache_append",
+                 "aif_cache_attend", "aif_cache_read", "aif_cache_fork", "aif_cache_copy", "aif_cache_free",
+                 "aif_cache_truncate", "aif_cache_trim", "aif_cache_compact", "aif_cache_swap_pool", "aif_cache_len",
+                 "aif_cache_free_pages")
+
+
+def _declare_cache(lib):
+    vp, i32 = C.c_void_p, C.c_int32
+    ids = C.POINTER(i32)
+    for name, res, args in (
+            ("aif_cache_page_bytes", C.c_size_t, [C.POINTER(aif_cache_config)]),
+            ("aif_cache_init", C.c_int, [C.POINTER(aif_cache_config), vp, C.POINTER(vp)]),
+            ("aif_cache_destroy", None, [vp]),
+            ("aif_cache_last_error", C.c_char_p, [vp]),
+            ("aif_cache_append", C.c_int, [vp, C.POINTER(aif_cache_append_req), i32, vp]),
+            ("aif_cache_attend", C.c_int, [vp, C.POINTER(aif_cache_attend_req), i32, vp]),
+            ("aif_cache_read", C.c_int, [vp, C.POINTER(aif_cache_read_req), i32, vp]),
+            ("aif_cache_fork", C.c_int, [vp, ids, ids, i32, vp]),
+            ("aif_cache_copy", C.c_int, [vp, ids, ids, i32, vp]),
+            ("aif_cache_free", C.c_int, [vp, ids, i32]),
+            ("aif_cache_truncate", C.c_int, [vp, i32, i32]),
+            ("aif_cache_trim", C.c_int, [vp, ids, i32, i32, i32, vp]),
+            ("aif_cache_compact", C.c_int, [vp, ids, vp]),
+            ("aif_cache_swap_pool", C.c_int, [vp, vp, i32]),
+            ("aif_cache_len", i32, [vp, i32]),
+            ("aif_cache_free_pages", i32, [vp])):
+        f = getattr(lib, name)
+        f.restype, f.argtypes = res, args
+
+
+def _row_stride(t, width: int) -> int:
+    """Elements from one row of [rows, ...] to the next; rows themselves lie close."""
+    if t is None or t.numel() == 0 or t.shape[0] == 1:
+        return 0
+    row = t[0]
+    if row.numel() != width or not row.is_contiguous():
+        raise ValueError(f"a row of {width} contiguous features is wanted, got {tuple(row.shape)} with strides {row.stride()}")
+    return int(t.stride(0))
+
+
+class CacheAppend:
+    """Rows for the end of a sequence: keys and vals [n_rows, n_kv_heads * d_head] (or [n_rows, n_kv_heads, d_head]), rows
+    that may lie apart."""
+
+    def __init__(self, seq: int, keys, vals):
+        self.seq, self.keys, self.vals = int(seq), keys, vals
+        self.n_rows = int(keys.shape[0])
+        if tuple(vals.shape) != tuple(keys.shape):
+            raise ValueError(f"keys {tuple(keys.shape)} and vals {tuple(vals.shape)} differ")
+        self.width = keys[0].numel() if self.n_rows else 0
+        self.strides = _row_stride(keys, self.width), _row_stride(vals, self.width)
+
+    def fill(self, r: aif_cache_append_req):
+        r.seq, r.n_rows, r.keys, r.vals = self.seq, self.n_rows, _ptr(self.keys), _ptr(self.vals)
+        r.key_stride, r.val_stride = self.strides
+
+
+class CacheQuery:
+    """Queries over a sequence: q and out [n_q, n_heads, d_head] (or [n_q, n_heads * d_head]), rows that may lie apart;
+    lse [n_q, n_heads] fp32 and positions [n_q] int32, both contiguous."""
+
+    def __init__(self, seq: int, q, out, lse=None, positions=None, sinks: int = 0, window: int = 0):
+        self.seq, self.q, self.out, self.lse, self.positions = int(seq), q, out, lse, positions
+        self.sinks, self.window = int(sinks), int(window)
+        self.n_q = int(q.shape[0])
+        if tuple(out.shape) != tuple(q.shape):
+            raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} differ")
+        for name, t, n in (("lse", lse, None), ("positions", positions, self.n_q)):
+            if t is not None and (t.shape[0] != self.n_q or not t.is_contiguous() or (n is not None and t.numel() != n)):
+                raise ValueError(f"{name}: contiguous, a row for each of {self.n_q} queries, got {tuple(t.shape)}")
+        self.width = q[0].numel() if self.n_q else 0
+        self.strides = _row_stride(q, self.width), _row_stride(out, self.width)
+
+    def fill(self, r: aif_cache_attend_req):
+        r.seq, r.n_q, r.q, r.out, r.lse_out, r.positions = self.seq, self.n_q, _ptr(self.q), _ptr(self.out), _ptr(self.lse), _ptr(self.positions)
+        r.q_stride, r.out_stride = self.strides
+        r.sinks, r.window = self.sinks, self.window
+
+
+class CacheRead:
+    """Rows [first, first + n_rows) of a sequence, to keys_out and vals_out [n_rows, ...] (either may be None)."""
+
+    def __init__(self, seq: int, keys_out, vals_out, first: int = 0):
+        self.seq, self.keys_out, self.vals_out, self.first = int(seq), keys_out, vals_out, int(first)
+        one = keys_out if keys_out is not None else vals_out
+        if one is None or (vals_out is not None and tuple(vals_out.shape) != tuple(one.shape)):
+            raise ValueError("keys_out or vals_out is wanted, of one shape")
+        self.n_rows = int(one.shape[0])
+        self.width = one[0].numel() if self.n_rows else 0
+        self.strides = _row_stride(keys_out, self.width), _row_stride(vals_out, self.width)
+
+    def fill(self, r: aif_cache_read_req):
+        r.seq, r.first, r.n_rows, r.reserved = self.seq, self.first, self.n_rows, 0
+        r.keys_out, r.vals_out = _ptr(self.keys_out), _ptr(self.vals_out)
+        r.key_stride, r.val_stride = self.strides
+
+
+def _pack_cache(kind, reqs):
+    arr = (kind * max(len(reqs), 1))()
+    for i, q in enumerate(reqs):
+        q.fill(arr[i])
+    return arr
+
+
+def pack_cache_appends(reqs: Sequence[CacheAppend]):
+    return _pack_cache(aif_cache_append_req, reqs)
+
+
+def pack_cache_queries(reqs: Sequence[CacheQuery]):
+    return _pack_cache(aif_cache_attend_req, reqs)
+
+
+def pack_cache_reads(reqs: Sequence[CacheRead]):
+    return _pack_cache(aif_cache_read_req, reqs)
+
+
+def cache_ids(seqs):
+    """Sequence numbers as the array the C entry points take; such an array is taken as it is."""
+    if isinstance(seqs, C.Array):
+        return seqs
+    seqs = [int(q) for q in seqs]
+    return (C.c_int32 * len(seqs))(*seqs)
+
+
+def cache_page_bytes(*, dtype: int, n_heads: int, n_kv_heads: int, d_head: int, page_len: int) -> int:
+    """Bytes of a page; the pool is n_pages of them."""
+    cfg = aif_cache_config(dtype, n_heads, n_kv_heads, d_head, 0.0, page_len, 0, 0, 0, 0, 0)
+    n = int(load().aif_cache_page_bytes(C.byref(cfg)))
+    if n == 0:
+        raise AifError(AIF_ESHAPE, load().aif_cache_last_error(None).decode())
+    return n
+
+
+class CacheContext:
+    """Owns one ``aif_cache_ctx`` over the pool (a uint8 tensor, borrowed).  Methods carry the names of the C entry points."""
+
+    def __init__(self, *, pool, dtype: int, n_heads: int, n_kv_heads: int, d_head: int, page_len: int, max_seqs: int,
+                 max_len: int, max_requests: int, max_queries: int = 1, scale: float = 0.0, n_pages: Optional[int] = None):
+        self._lib = load()
+        self._h = C.c_void_p()
+        self._page_bytes = cache_page_bytes(dtype=dtype, n_heads=n_heads, n_kv_heads=n_kv_heads, d_head=d_head, page_len=page_len)
+        have = pool.numel() * pool.element_size() // self._page_bytes
+        n_pages = have if n_pages is None else n_pages
+        if n_pages > have:
+            raise ValueError(f"the pool holds {have} pages, not {n_pages}")
+        self._kv_width, self._q_width = n_kv_heads * d_head, n_heads * d_head
+        self.n_heads, self.dtype = n_heads, dtype
+        cfg = aif_cache_config(dtype, n_heads, n_kv_heads, d_head, scale, page_len, n_pages, max_seqs, max_len, max_requests, max_queries)
+        self._keep = (pool,)                       # borrowed for the life of the context
+        st = self._lib.aif_cache_init(C.byref(cfg), _ptr(pool), C.byref(self._h))
+        if st != AIF_OK:
+            self._h = C.c_void_p()
+            raise AifError(st, self._lib.aif_cache_last_error(None).decode())
+
+    def _check(self, st: int):
+        if st != AIF_OK:
+            raise AifError(st, self._lib.aif_cache_last_error(self._h).decode())
+
+    def _packed(self, reqs, packed, pack, width, *tensors):
+        """The packed array; requests that are packed here are held against the context's row width and type first."""
+        if packed is not None:
+            return packed
+        import torch
+        want = torch.float32 if self.dtype == AIF_F32 else torch.bfloat16
+        for i, r in enumerate(reqs):
+            for name in tensors:
+                t = getattr(r, name)
+                if t is not None and t.numel() and (t.dtype != want or r.width != width):
+                    raise ValueError(f"request {i}: {name} has rows of {r.width} {t.dtype}, the context {width} {want}")
+        return pack(reqs)
+
+    def aif_cache_append(self, reqs: Sequence[CacheAppend], packed=None):
+        arr = self._packed(reqs, packed, pack_cache_appends, self._kv_width, "keys", "vals")
+        self._check(self._lib.aif_cache_append(self._h, arr, len(reqs), _stream()))
+
+    def aif_cache_attend(self, reqs: Sequence[CacheQuery], packed=None):
+        arr = self._packed(reqs, packed, pack_cache_queries, self._q_width, "q", "out")
+        if packed is None:
+            import torch
+            for i, r in enumerate(reqs):
+                if r.lse is not None and (r.lse.dtype != torch.float32 or r.lse.numel() != r.n_q * self.n_heads):
+                    raise ValueError(f"request {i}: lse is [n_q, {self.n_heads}] fp32")
+                if r.positions is not None and r.positions.dtype != torch.int32:
+                    raise ValueError(f"request {i}: positions are int32")
+        self._check(self._lib.aif_cache_attend(self._h, arr, len(reqs), _stream()))
+
+    def aif_cache_read(self, reqs: Sequence[CacheRead], packed=None):
+        arr = self._packed(reqs, packed, pack_cache_reads, self._kv_width, "keys_out", "vals_out")
+        self._check(self._lib.aif_cache_read(self._h, arr, len(reqs), _stream()))
+
+    def _pairs(self, src, dst):
+        src, dst = cache_ids(src), cache_ids(dst)
+        if len(src) != len(dst):
+            raise ValueError(f"{len(src)} sources and {len(dst)} destinations")
+        return src, dst, len(src), _stream()
+
+    def aif_cache_fork(self, src, dst):
+        self._check(self._lib.aif_cache_fork(self._h, *self._pairs(src, dst)))
+
+    def aif_cache_copy(self, src, dst):
+        self._check(self._lib.aif_cache_copy(self._h, *self._pairs(src, dst)))
+
+    def aif_cache_free(self, seqs):
+        seqs = cache_ids(seqs)
+        self._check(self._lib.aif_cache_free(self._h, seqs, len(seqs)))
+
+    def aif_cache_truncate(self, seq: int, length: int):
+        self._check(self._lib.aif_cache_truncate(self._h, seq, length))
+
+    def aif_cache_trim(self, seqs, sinks: int, window: int):
+        seqs = cache_ids(seqs)
+        self._check(self._lib.aif_cache_trim(self._h, seqs, len(seqs), sinks, window, _stream()))
+
+    def aif_cache_compact(self) -> int:
+        n = C.c_int32(0)
+        self._check(self._lib.aif_cache_compact(self._h, C.byref(n), _stream()))
+        return n.value
+
+    def aif_cache_swap_pool(self, pool, n_pages: Optional[int] = None):
+        have = pool.numel() * pool.element_size() // self._page_bytes
+        if n_pages is not None and n_pages > have:
+            raise ValueError(f"the pool holds {have} pages, not {n_pages}")
+        self._check(self._lib.aif_cache_swap_pool(self._h, _ptr(pool), have if n_pages is None else n_pages))
+        self._keep = self._keep + (pool,)          # the old pool may still be read by enqueued work
+
+    def aif_cache_len(self, seq: int) -> int:
+        return int(self._lib.aif_cache_len(self._h, seq))
+
+    def aif_cache_free_pages(self) -> int:
+        return int(self._lib.aif_cache_free_pages(self._h))
+
+    def close(self):
+        if self._h:
+            self._lib.aif_cache_destroy(self._h)
             self._h = C.c_void_p()
 
     def __del__(self):

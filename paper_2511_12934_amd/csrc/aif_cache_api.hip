@@ -1,0 +1,542 @@
+// C ABI of the user cache (include/aif_cache.h): context, validation, which pages belong to which sequence, and the launches.
+//
+// The host's book-keeping is what counts: every call settles at once which pages it takes and gives back, and the device's
+// copy of the page table follows on the stream with the launches that need it.  A call checks everything first; from there on
+// only a HIP call can fail.  Nothing is allocated after aif_cache_init.
+#include "../../include/aif_cache.h"
+#include "aif_cache_dev.h"
+#include "cache_book.h"
+
+#include <algorithm>
+#include <cstdarg>
+#include <cstdio>
+#include <exception>
+#include <new>
+#include <vector>
+
+using namespace aif;
+
+namespace {
+constexpr int CACHE_NSLOT = 8;
+constexpr size_t CACHE_SLOT_BYTES = 64 << 10;
+constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
+thread_local char g_cache_init_error[512] = "";
+}  // namespace
+
+struct aif_cache_ctx {
+    CacheShape shape{};
+    aif_cache_config cfg{};
+    int device = 0;
+    CacheBook book;
+    std::vector<uint32_t> stamp;            // sequences that a call has named
+    uint32_t stamp_now = 0;
+    char *h_stage = nullptr, *h_stage_dev = nullptr;
+    char *d_stage = nullptr;
+    size_t slot_bytes = CACHE_SLOT_BYTES;
+    hipEvent_t ev[CACHE_NSLOT] = {};
+    bool ev_live[CACHE_NSLOT] = {};
+    int next_slot = 0;
+    alignas(16) char few[CACHE_FEW_BYTES];
+    char err[512] = "";
+};
+
+namespace {
+
+aif_status cfail(aif_cache_ctx *c, aif_status st, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(c ? c->err : g_cache_init_error, 512, fmt, ap);
+    va_end(ap);
+    return st;
+}
+
+#define CACHE_TRY(ctxp, expr)                                                                         \
+    do {                                                                                              \
+        hipError_t e_ = (expr);                                                                       \
+        if (e_ != hipSuccess)                                                                         \
+            return cfail(ctxp, e_ == hipErrorOutOfMemory ? AIF_ENOMEM : AIF_EDEVICE, "%s: %s", #expr, \
+                         hipGetErrorString(e_));                                                      \
+    } while (0)
+
+aif_status check_config(const aif_cache_config *f)
+{
+    if (f->dtype != AIF_F32 && f->dtype != AIF_BF16) return cfail(nullptr, AIF_EINVAL, "unknown dtype %d", (int)f->dtype);
+    if (f->n_heads <= 0 || f->n_kv_heads <= 0 || f->d_head <= 0) return cfail(nullptr, AIF_EINVAL, "non-positive head count or width");
+    if (f->n_heads % f->n_kv_heads) return cfail(nullptr, AIF_ESHAPE, "n_heads %d is not a multiple of n_kv_heads %d", f->n_heads, f->n_kv_heads);
+    if (f->n_heads > 65535) return cfail(nullptr, AIF_ESHAPE, "n_heads %d is above 65535", f->n_heads);
+    const int vec = f->dtype == AIF_F32 ? 4 : 8;
+    if (f->d_head % vec || f->d_head > CACHE_MAX_DP) return cfail(nullptr, AIF_ESHAPE, "d_head %d is not a multiple of %d up to %d", f->d_head, vec, CACHE_MAX_DP);
+    if (f->page_len < CACHE_TILE || f->page_len > 1024 || f->page_len % CACHE_TILE)
+        return cfail(nullptr, AIF_ESHAPE, "page_len %d is not a multiple of %d up to 1024", f->page_len, CACHE_TILE);
+    return AIF_OK;
+}
+
+bool name_once(aif_cache_ctx *c, int seq)
+{
+    if (c->stamp[seq] == c->stamp_now) return false;
+    c->stamp[seq] = c->stamp_now;
+    return true;
+}
+void name_none(aif_cache_ctx *c)
+{
+    if (++c->stamp_now == 0) {
+        std::fill(c->stamp.begin(), c->stamp.end(), 0u);
+        c->stamp_now = 1;
+    }
+}
+
+aif_status check_seq(aif_cache_ctx *c, const char *what, int i, int seq)
+{
+    if (seq < 0 || seq >= c->cfg.max_seqs) return cfail(c, AIF_ERANGE, "%s %d: sequence %d is outside 0..%d", what, i, seq, c->cfg.max_seqs - 1);
+    return AIF_OK;
+}
+
+aif_status check_count(aif_cache_ctx *c, const void *array, int32_t n, int32_t most)
+{
+    if (n < 0 || (n > 0 && !array)) return cfail(c, AIF_EINVAL, "NULL array or negative count");
+    if (n > most) return cfail(c, AIF_ERANGE, "%d entries, the context takes %d", n, most);
+    return AIF_OK;
+}
+
+aif_status check_tensor(aif_cache_ctx *c, const char *what, int i, const void *p, int64_t stride, int width)
+{
+    const int vec = c->shape.dtype == 0 ? 4 : 8;
+    if (!p) return cfail(c, AIF_EINVAL, "%s %d: NULL tensor pointer", what, i);
+    if ((uintptr_t)p % 16 || stride % vec) return cfail(c, AIF_EINVAL, "%s %d: tensors and strides must be multiples of 16 bytes", what, i);
+    if (stride != 0 && (stride < width || stride > (int64_t)1 << 40)) return cfail(c, AIF_EINVAL, "%s %d: stride %lld below the row's %d", what, i, (long long)stride, width);
+    return AIF_OK;
+}
+
+// The device is the context's and the stream is not being captured.
+aif_status check_stream(aif_cache_ctx *c, hipStream_t s)
+{
+    int cur = -1;
+    CACHE_TRY(c, hipGetDevice(&cur));
+    if (cur != c->device) return cfail(c, AIF_EDEVICE, "context belongs to device %d, current device is %d", c->device, cur);
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(s, &st) != hipSuccess) {       // the default stream while another one is captured
+        (void)hipGetLastError();
+        st = hipStreamCaptureStatusActive;
+    }
+    if (st != hipStreamCaptureStatusNone) return cfail(c, AIF_EINVAL, "the stream is being captured: this call cannot be");
+    return AIF_OK;
+}
+
+// A list of descriptors on its way to a launch.  Up to CACHE_FEW_BYTES of a call travel in the kernel's arguments; more are
+// cut into lists of a slot of the pinned ring each, uploaded on the stream.
+template <class T> class CacheBatch {
+public:
+    CacheBatch(aif_cache_ctx *c, size_t expected, hipStream_t s) : c_(c), s_(s), far_(expected * sizeof(T) > CACHE_FEW_BYTES) {}
+    // go: launches the list
+    template <class F> aif_status add(const T &t, F &&go)
+    {
+        const size_t room = (far_ ? CACHE_SLOT_BYTES : (size_t)CACHE_FEW_BYTES) / sizeof(T);
+        if (n_ == (int)room) {
+            const aif_status st = send(go);
+            if (st != AIF_OK) return st;
+        }
+        if (n_ == 0) {
+            if (far_) {
+                slot_ = c_->next_slot;
+                if (c_->ev_live[slot_]) CACHE_TRY(c_, hipEventSynchronize(c_->ev[slot_]));
+                c_->ev_live[slot_] = false;
+                c_->next_slot = (slot_ + 1) % CACHE_NSLOT;
+                at_ = (T *)(c_->h_stage + (size_t)slot_ * c_->slot_bytes);
+            } else
+                at_ = (T *)c_->few;
+        }
+        at_[n_++] = t;
+        return AIF_OK;
+    }
+    template <class F> aif_status send(F &&go)
+    {
+        if (n_ == 0) return AIF_OK;
+        CacheList l{at_, nullptr, n_, (size_t)n_ * sizeof(T)};
+        n_ = 0;
+        if (far_) {
+            const size_t off = (size_t)slot_ * c_->slot_bytes;
+            CACHE_TRY(c_, staging_upload(c_->h_stage, c_->h_stage_dev, off, c_->d_stage + off, l.bytes, s_));
+            l.dev = c_->d_stage + off;
+        }
+        CACHE_TRY(c_, go(l));
+        if (far_) {
+            CACHE_TRY(c_, hipEventRecord(c_->ev[slot_], s_));
+            c_->ev_live[slot_] = true;
+        }
+        return AIF_OK;
+    }
+
+private:
+    aif_cache_ctx *c_;
+    hipStream_t s_;
+    bool far_;
+    T *at_ = nullptr;
+    int n_ = 0, slot_ = 0;
+};
+
+void cdestroy(aif_cache_ctx *c)
+{
+    if (!c) return;
+    if (c->shape.table) (void)hipFree(c->shape.table);
+    if (c->d_stage) (void)hipFree(c->d_stage);
+    if (c->h_stage) (void)hipHostFree(c->h_stage);
+    for (int i = 0; i < CACHE_NSLOT; ++i)
+        if (c->ev[i]) (void)hipEventDestroy(c->ev[i]);
+    delete c;
+}
+
+aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
+{
+    const aif_status st = check_config(f);
+    if (st != AIF_OK) return st;
+    if (f->n_pages <= 0 || f->max_seqs <= 0 || f->max_len <= 0 || f->max_requests <= 0 || f->max_queries <= 0)
+        return cfail(nullptr, AIF_EINVAL, "non-positive size in aif_cache_config");
+    if (f->max_requests > 65535) return cfail(nullptr, AIF_ESHAPE, "max_requests %d is above 65535", f->max_requests);
+    if (!(f->scale == f->scale) || f->scale - f->scale != 0.f) return cfail(nullptr, AIF_EINVAL, "scale is not finite");
+    if (!pool || (uintptr_t)pool % 64) return cfail(nullptr, AIF_EINVAL, "the pool is NULL or not 64-byte aligned");
+    c->cfg = *f;
+    CacheShape &s = c->shape;
+    s.pool = (char *)pool;
+    s.page_bytes = aif_cache_page_bytes(f);
+    s.n_heads = f->n_heads;
+    s.n_kv = f->n_kv_heads;
+    s.group = f->n_heads / f->n_kv_heads;
+    s.d_head = f->d_head;
+    s.dp = (f->d_head + CACHE_BLOCK - 1) / CACHE_BLOCK * CACHE_BLOCK;
+    s.page_len = f->page_len;
+    s.dtype = f->dtype == AIF_F32 ? 0 : 1;
+    s.scale = f->scale != 0.f ? f->scale : 1.0f / __builtin_sqrtf((float)f->d_head);
+    s.pages_per_seq = (int)(((int64_t)f->max_len + f->page_len - 1) / f->page_len);
+    const int64_t entries = (int64_t)f->max_seqs * s.pages_per_seq;
+    if (entries > INT32_MAX / 2) return cfail(nullptr, AIF_ESHAPE, "max_seqs * max_len / page_len = %lld table entries are too many", (long long)entries);
+    c->book.init(f->max_seqs, f->max_len, f->page_len, f->n_pages);
+    c->stamp.assign(f->max_seqs, 0u);
+    CACHE_TRY(nullptr, hipGetDevice(&c->device));
+    CACHE_TRY(nullptr, hipMalloc((void **)&s.table, (size_t)entries * sizeof(int32_t)));
+    // a list of asks is one upload, whatever its length
+    const size_t asks = (size_t)f->max_requests * (sizeof(CacheAsk) + sizeof(int32_t)) + 64;
+    c->slot_bytes = ((asks > CACHE_SLOT_BYTES ? asks : CACHE_SLOT_BYTES) + 255) / 256 * 256;
+    CACHE_TRY(nullptr, staging_alloc(c->slot_bytes * CACHE_NSLOT, &c->h_stage, &c->h_stage_dev));
+    CACHE_TRY(nullptr, hipMalloc((void **)&c->d_stage, c->slot_bytes * CACHE_NSLOT));
+    for (int i = 0; i < CACHE_NSLOT; ++i)
+        CACHE_TRY(nullptr, hipEventCreateWithFlags(&c->ev[i], hipEventDisableTiming | hipEventDisableSystemFence));
+    return AIF_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t aif_cache_page_bytes(const aif_cache_config *f)
+{
+    if (!f || check_config(f) != AIF_OK) return 0;
+    const int dp = (f->d_head + CACHE_BLOCK - 1) / CACHE_BLOCK * CACHE_BLOCK;
+    return (size_t)f->n_kv_heads * (f->page_len / CACHE_TILE) * cache_tile_bytes(dp);
+}
+
+aif_status aif_cache_init(const aif_cache_config *cfg, void *pool, aif_cache_ctx **out)
+{
+    if (!cfg || !out) return cfail(nullptr, AIF_EINVAL, "NULL argument");
+    aif_cache_ctx *c = new (std::nothrow) aif_cache_ctx();
+    if (!c) return cfail(nullptr, AIF_ENOMEM, "out of host memory");
+    aif_status st;
+    try {
+        st = cinit(cfg, pool, c);
+    } catch (const std::exception &) {
+        st = cfail(nullptr, AIF_ENOMEM, "out of host memory");
+    }
+    if (st != AIF_OK) {
+        cdestroy(c);
+        return st;
+    }
+    *out = c;
+    return AIF_OK;
+}
+
+void aif_cache_destroy(aif_cache_ctx *ctx) { cdestroy(ctx); }
+
+const char *aif_cache_last_error(const aif_cache_ctx *ctx) { return ctx ? ctx->err : g_cache_init_error; }
+
+int32_t aif_cache_len(const aif_cache_ctx *ctx, int32_t seq) { return !ctx || seq < 0 || seq >= ctx->cfg.max_seqs ? -1 : ctx->book.len(seq); }
+
+int32_t aif_cache_free_pages(const aif_cache_ctx *ctx) { return ctx ? ctx->book.n_free : -1; }
+
+// about the runs that n rows are cut into
+static int64_t runs_of(int64_t n, int page_len) { return n == 0 ? 0 : 1 + n / UNIT_ROWS + n / page_len; }
+
+aif_status aif_cache_append(aif_cache_ctx *c, const aif_cache_append_req *reqs, int32_t n, void *hip_stream)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_count(c, reqs, n, c->cfg.max_requests);
+    if (st != AIF_OK) return st;
+    const int width = c->shape.n_kv * c->shape.d_head, pl = c->cfg.page_len;
+    int64_t pages = 0, units = 0;
+    name_none(c);
+    for (int r = 0; r < n; ++r) {
+        const aif_cache_append_req &q = reqs[r];
+        if ((st = check_seq(c, "append", r, q.seq)) != AIF_OK) return st;
+        if (!name_once(c, q.seq)) return cfail(c, AIF_EINVAL, "append %d: sequence %d is named twice", r, q.seq);
+        if (q.n_rows < 0) return cfail(c, AIF_EINVAL, "append %d: negative n_rows", r);
+        if (q.n_rows > 0 && ((st = check_tensor(c, "append", r, q.keys, q.key_stride, width)) != AIF_OK ||
+                             (st = check_tensor(c, "append", r, q.vals, q.val_stride, width)) != AIF_OK))
+            return st;
+        const int len = c->book.len(q.seq);
+        if (q.n_rows > c->cfg.max_len - len) return cfail(c, AIF_ERANGE, "append %d: %d rows behind %d exceed max_len %d", r, q.n_rows, len, c->cfg.max_len);
+        pages += c->book.append_needs(q.seq, q.n_rows);
+        units += runs_of(q.n_rows, pl);
+    }
+    if (pages > c->book.n_free) return cfail(c, AIF_ERANGE, "%lld pages needed, %d are free", (long long)pages, c->book.n_free);
+    hipStream_t s = (hipStream_t)hip_stream;
+    if ((st = check_stream(c, s)) != AIF_OK) return st;
+
+    CacheBatch<CacheUnit> batch(c, (size_t)units, s);
+    auto go = [&](const CacheList &l) { return launch_cache_append(c->shape, l, s); };
+    const int esz = c->shape.dtype == 0 ? 4 : 2;
+    for (int r = 0; r < n && st == AIF_OK; ++r) {
+        const aif_cache_append_req &q = reqs[r];
+        const int64_t ks = q.key_stride ? q.key_stride : width, vs = q.val_stride ? q.val_stride : width;
+        c->book.append(q.seq, q.n_rows, UNIT_ROWS, [&](int32_t done, int32_t i, int32_t cow, int32_t row0, int32_t rows) {
+            const CacheUnit u{(const char *)q.keys + done * ks * esz, (const char *)q.vals + done * vs * esz, ks, vs, c->book.page(q.seq, i), cow,
+                              row0, rows, c->book.entry(q.seq, i), 0};
+            if (st == AIF_OK) st = batch.add(u, go);
+        });
+    }
+    if (st == AIF_OK) st = batch.send(go);
+    c->book.settle();
+    return st;
+}
+
+aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int32_t n, void *hip_stream)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_count(c, reqs, n, c->cfg.max_requests);
+    if (st != AIF_OK) return st;
+    const int width = c->shape.n_kv * c->shape.d_head, pl = c->cfg.page_len;
+    int64_t units = 0;
+    for (int r = 0; r < n; ++r) {
+        const aif_cache_read_req &q = reqs[r];
+        if ((st = check_seq(c, "read", r, q.seq)) != AIF_OK) return st;
+        if (q.n_rows < 0 || q.first < 0 || q.reserved) return cfail(c, AIF_EINVAL, "read %d: negative rows, or reserved is not 0", r);
+        if (q.first > c->book.len(q.seq) || q.n_rows > c->book.len(q.seq) - q.first)
+            return cfail(c, AIF_ERANGE, "read %d: rows %d.. of %d, the sequence has %d", r, q.first, q.n_rows, c->book.len(q.seq));
+        if (q.n_rows == 0) continue;
+        if ((q.keys_out && (st = check_tensor(c, "read", r, q.keys_out, q.key_stride, width)) != AIF_OK) ||
+            (q.vals_out && (st = check_tensor(c, "read", r, q.vals_out, q.val_stride, width)) != AIF_OK))
+            return st;
+        for (int p = q.first / pl; p <= (q.first + q.n_rows - 1) / pl; ++p)
+            if (c->book.page(q.seq, p) < 0) return cfail(c, AIF_ERANGE, "read %d: rows from %d on were dropped", r, p * pl);
+        units += runs_of(q.n_rows, pl);
+    }
+    hipStream_t s = (hipStream_t)hip_stream;
+    if ((st = check_stream(c, s)) != AIF_OK) return st;
+    CacheBatch<CacheUnit> batch(c, (size_t)units, s);
+    auto go = [&](const CacheList &l) { return launch_cache_read(c->shape, l, s); };
+    const int esz = c->shape.dtype == 0 ? 4 : 2;
+    for (int r = 0; r < n; ++r) {
+        const aif_cache_read_req &q = reqs[r];
+        const int64_t ks = q.key_stride ? q.key_stride : width, vs = q.val_stride ? q.val_stride : width;
+        if (!q.keys_out && !q.vals_out) continue;
+        for (int done = 0; done < q.n_rows;) {
+            const int at = q.first + done, row0 = at % pl;
+            const int rows = std::min({UNIT_ROWS - row0 % UNIT_ROWS, pl - row0, q.n_rows - done});
+            const CacheUnit u{q.keys_out ? (const char *)q.keys_out + done * ks * esz : nullptr,
+                              q.vals_out ? (const char *)q.vals_out + done * vs * esz : nullptr, ks, vs, c->book.page(q.seq, at / pl), -1, row0, rows, 0, 0};
+            done += rows;
+            if ((st = batch.add(u, go)) != AIF_OK) return st;
+        }
+    }
+    return batch.send(go);
+}
+
+aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, int32_t n, void *hip_stream)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_count(c, reqs, n, c->cfg.max_requests);
+    if (st != AIF_OK) return st;
+    const int width = c->shape.n_heads * c->shape.d_head, esz = c->shape.dtype == 0 ? 4 : 2;
+    int64_t rows = 0;
+    for (int r = 0; r < n; ++r) {
+        const aif_cache_attend_req &q = reqs[r];
+        if ((st = check_seq(c, "attend", r, q.seq)) != AIF_OK) return st;
+        if (q.n_q < 0 || q.sinks < 0 || q.window < 0) return cfail(c, AIF_EINVAL, "attend %d: negative n_q, sinks or window", r);
+        if (q.n_q > c->cfg.max_queries) return cfail(c, AIF_ERANGE, "attend %d: n_q %d exceeds max_queries %d", r, q.n_q, c->cfg.max_queries);
+        if (q.n_q > 0 && ((st = check_tensor(c, "attend", r, q.q, q.q_stride, width)) != AIF_OK ||
+                          (st = check_tensor(c, "attend", r, q.out, q.out_stride, width)) != AIF_OK))
+            return st;
+        if (((uintptr_t)q.lse_out | (uintptr_t)q.positions) % 4) return cfail(c, AIF_EINVAL, "attend %d: lse_out and positions must be 4-byte aligned", r);
+        rows += q.n_q;
+    }
+    if (rows > INT32_MAX) return cfail(c, AIF_ERANGE, "%lld queries in one call are too many", (long long)rows);
+    hipStream_t s = (hipStream_t)hip_stream;
+    if ((st = check_stream(c, s)) != AIF_OK) return st;
+    if (rows == 0) return AIF_OK;
+
+    const size_t bytes = (size_t)n * sizeof(CacheAsk) + ((size_t)n + 1) * sizeof(int32_t);
+    const bool far = bytes > CACHE_FEW_BYTES;
+    int slot = 0;
+    char *h = c->few;
+    if (far) {
+        slot = c->next_slot;
+        if (c->ev_live[slot]) CACHE_TRY(c, hipEventSynchronize(c->ev[slot]));
+        c->ev_live[slot] = false;
+        c->next_slot = (slot + 1) % CACHE_NSLOT;
+        h = c->h_stage + (size_t)slot * c->slot_bytes;
+    }
+    CacheAsk *ha = (CacheAsk *)h;
+    int32_t *first = (int32_t *)(h + (size_t)n * sizeof(CacheAsk));
+    int32_t at = 0;
+    for (int r = 0; r < n; ++r) {
+        const aif_cache_attend_req &q = reqs[r];
+        first[r] = at;
+        at += q.n_q;
+        ha[r] = CacheAsk{(const char *)q.q, (char *)q.out, q.lse_out, q.positions, (q.q_stride ? q.q_stride : width) * esz,
+                         (q.out_stride ? q.out_stride : width) * esz, q.n_q, c->book.len(q.seq), q.sinks, q.window, c->book.entry(q.seq, 0), 0};
+    }
+    first[n] = at;
+    CacheList l{h, nullptr, n, bytes};
+    if (far) {
+        const size_t off = (size_t)slot * c->slot_bytes;
+        CACHE_TRY(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
+        l.dev = c->d_stage + off;
+    }
+    CACHE_TRY(c, launch_cache_attend(c->shape, l, rows, s));
+    if (far) {
+        CACHE_TRY(c, hipEventRecord(c->ev[slot], s));
+        c->ev_live[slot] = true;
+    }
+    return AIF_OK;
+}
+
+// what fork and copy ask of their arguments
+static aif_status check_branches(aif_cache_ctx *c, const char *what, const int32_t *src, const int32_t *dst, int32_t n)
+{
+    aif_status st = check_count(c, src, n, c->cfg.max_seqs);
+    if (st == AIF_OK) st = check_count(c, dst, n, c->cfg.max_seqs);
+    if (st != AIF_OK) return st;
+    name_none(c);
+    for (int i = 0; i < n; ++i) {
+        if ((st = check_seq(c, what, i, src[i])) != AIF_OK || (st = check_seq(c, what, i, dst[i])) != AIF_OK) return st;
+        if (c->book.len(dst[i])) return cfail(c, AIF_EINVAL, "%s %d: sequence %d is not empty", what, i, dst[i]);
+        if (!name_once(c, dst[i])) return cfail(c, AIF_EINVAL, "%s %d: sequence %d is named twice", what, i, dst[i]);
+    }
+    for (int i = 0; i < n; ++i)
+        if (c->stamp[src[i]] == c->stamp_now) return cfail(c, AIF_EINVAL, "%s %d: sequence %d is source and destination", what, i, src[i]);
+    return AIF_OK;
+}
+
+aif_status aif_cache_fork(aif_cache_ctx *c, const int32_t *src, const int32_t *dst, int32_t n, void *hip_stream)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_branches(c, "fork", src, dst, n);
+    if (st != AIF_OK) return st;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if ((st = check_stream(c, s)) != AIF_OK) return st;
+    int longest = 0;
+    for (int i = 0; i < n; ++i) longest = std::max(longest, c->book.pages(c->book.len(src[i])));
+    CacheBatch<CacheFill> batch(c, (size_t)n, s);
+    auto go = [&](const CacheList &l) { return launch_cache_fill(c->shape, l, longest, s); };
+    for (int i = 0; i < n && st == AIF_OK; ++i) {
+        c->book.fork(src[i], dst[i]);
+        const int np = c->book.pages(c->book.len(src[i]));
+        if (np) st = batch.add(CacheFill{c->book.entry(dst[i], 0), np, c->book.entry(src[i], 0), 0}, go);
+    }
+    return st == AIF_OK ? batch.send(go) : st;
+}
+
+aif_status aif_cache_copy(aif_cache_ctx *c, const int32_t *src, const int32_t *dst, int32_t n, void *hip_stream)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_branches(c, "copy", src, dst, n);
+    if (st != AIF_OK) return st;
+    int64_t pages = 0, entries = 0;
+    for (int i = 0; i < n; ++i) {
+        pages += c->book.copy_needs(src[i]);
+        entries += c->book.pages(c->book.len(src[i]));
+    }
+    if (pages > c->book.n_free) return cfail(c, AIF_ERANGE, "%lld pages needed, %d are free", (long long)pages, c->book.n_free);
+    hipStream_t s = (hipStream_t)hip_stream;
+    if ((st = check_stream(c, s)) != AIF_OK) return st;
+    CacheBatch<CacheMove> batch(c, (size_t)entries, s);
+    auto go = [&](const CacheList &l) { return launch_cache_move(c->shape, l, s); };
+    for (int i = 0; i < n && st == AIF_OK; ++i)
+        c->book.copy(src[i], dst[i], [&](int32_t p, int32_t from, int32_t to) {
+            if (st == AIF_OK) st = batch.add(CacheMove{from, to, c->book.entry(dst[i], p)}, go);
+        });
+    return st == AIF_OK ? batch.send(go) : st;
+}
+
+aif_status aif_cache_free(aif_cache_ctx *c, const int32_t *seqs, int32_t n)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_count(c, seqs, n, INT32_MAX);
+    if (st != AIF_OK) return st;
+    for (int i = 0; i < n; ++i)
+        if ((st = check_seq(c, "free", i, seqs[i])) != AIF_OK) return st;
+    for (int i = 0; i < n; ++i) c->book.truncate(seqs[i], 0);
+    return AIF_OK;
+}
+
+aif_status aif_cache_truncate(aif_cache_ctx *c, int32_t seq, int32_t len)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_seq(c, "truncate", 0, seq);
+    if (st != AIF_OK) return st;
+    if (len < 0 || len > c->book.len(seq)) return cfail(c, AIF_ERANGE, "truncate: length %d of %d", len, c->book.len(seq));
+    if (!c->book.truncate(seq, len)) return cfail(c, AIF_ERANGE, "truncate: row %d lies in a page that was dropped", len);
+    return AIF_OK;
+}
+
+aif_status aif_cache_trim(aif_cache_ctx *c, const int32_t *seqs, int32_t n, int32_t sinks, int32_t window, void *hip_stream)
+{
+    if (!c) return AIF_EINVAL;
+    aif_status st = check_count(c, seqs, n, INT32_MAX);
+    if (st != AIF_OK) return st;
+    if (sinks < 0 || window < 1) return cfail(c, AIF_EINVAL, "trim: sinks %d, window %d", sinks, window);
+    for (int i = 0; i < n; ++i)
+        if ((st = check_seq(c, "trim", i, seqs[i])) != AIF_OK) return st;
+    hipStream_t s = (hipStream_t)hip_stream;
+    if ((st = check_stream(c, s)) != AIF_OK) return st;
+    CacheBatch<CacheFill> batch(c, (size_t)n, s);
+    auto go = [&](const CacheList &l) { return launch_cache_fill(c->shape, l, c->shape.pages_per_seq, s); };
+    for (int i = 0; i < n && st == AIF_OK; ++i) {
+        int lo, hi;
+        c->book.trim(seqs[i], sinks, window, lo, hi);
+        if (lo < hi) st = batch.add(CacheFill{c->book.entry(seqs[i], lo), hi - lo, -1, -1}, go);
+    }
+    return st == AIF_OK ? batch.send(go) : st;
+}
+
+aif_status aif_cache_compact(aif_cache_ctx *c, int32_t *n_used, void *hip_stream)
+{
+    if (!c) return AIF_EINVAL;
+    hipStream_t s = (hipStream_t)hip_stream;
+    aif_status st = check_stream(c, s);
+    if (st != AIF_OK) return st;
+    const int64_t pages = c->book.out_of_place();
+    if (pages) {
+        // contents and names in one list: a page is copied before its new number is read, by launches that come later
+        CacheBatch<CacheMove> batch(c, (size_t)pages * 2, s);
+        auto go = [&](const CacheList &l) { return launch_cache_move(c->shape, l, s); };
+        c->book.compact([&](int32_t from, int32_t to) { if (st == AIF_OK) st = batch.add(CacheMove{from, to, -1}, go); },
+                        [&](int32_t q, int32_t i, int32_t to) { if (st == AIF_OK) st = batch.add(CacheMove{-1, to, c->book.entry(q, i)}, go); });
+        if (st == AIF_OK) st = batch.send(go);
+    }
+    if (n_used) *n_used = c->book.n_pages - c->book.n_free;
+    return st;
+}
+
+aif_status aif_cache_swap_pool(aif_cache_ctx *c, void *pool, int32_t n_pages)
+{
+    if (!c) return AIF_EINVAL;
+    if (!pool || (uintptr_t)pool % 64 || n_pages < 1) return cfail(c, AIF_EINVAL, "the pool is NULL or not 64-byte aligned, or has no pages");
+    try {
+        if (!c->book.set_pool(n_pages)) return cfail(c, AIF_ERANGE, "a page at or beyond %d is in use", n_pages);
+    } catch (const std::exception &) {
+        return cfail(c, AIF_ENOMEM, "out of host memory");
+    }
+    c->shape.pool = (char *)pool;
+    return AIF_OK;
+}
+
+}  // extern "C"

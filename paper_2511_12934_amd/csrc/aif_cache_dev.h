@@ -1,0 +1,91 @@
+// Internal device-side types and launcher prototypes of the user cache of libaif (gfx950 only).
+#pragma once
+#include "aif_dev.h"
+
+namespace aif {
+
+// A page holds page_len rows of one sequence, head after head, a head's rows in tiles of 32:
+//   keys' codes [32][dp / 2] | values' codes [32][dp / 2] | keys' scale bytes [32][dp / 32] | values' scale bytes [32][dp / 32]
+// with dp = d_head rounded up to blocks of 32 features (zeros past d_head), two codes a byte, the even feature low.
+// A tile is one address and 34 dp contiguous bytes: what a wave reads for 32 keys and values.
+constexpr int CACHE_TILE = 32;
+constexpr int CACHE_BLOCK = 32;
+constexpr int CACHE_MAX_DP = 256;
+constexpr int CACHE_E_MIN = -125, CACHE_E_MAX = 125;    // every value is a normal bf16: no flush, no overflow
+constexpr int CACHE_NAN = 255;
+
+struct CacheShape {
+    char *pool;
+    int32_t *table;             // [max_seqs, pages_per_seq]: pages of each sequence, -1 = dropped
+    size_t page_bytes;
+    int32_t n_heads, n_kv, group, d_head, dp, page_len, pages_per_seq, dtype;
+    float scale;
+};
+__host__ __device__ inline size_t cache_tile_bytes(int dp) { return (size_t)34 * dp; }
+__host__ __device__ inline size_t cache_head_bytes(const CacheShape &c) { return (size_t)(c.page_len / CACHE_TILE) * 34 * c.dp; }
+
+// Rows [row0, row0 + n) of one page, from keys and vals on (strides in elements).
+struct CacheUnit {
+    const char *keys, *vals;
+    int64_t key_stride, val_stride;
+    int32_t page, cow;          // cow >= 0: the page's rows before row0 come from that page first
+    int32_t row0, n;
+    int32_t entry, pad_;        // the table entry that names the page
+};
+// Table entries [dst, dst + n): those at src, or `value` where src < 0.
+struct CacheFill {
+    int32_t dst, n, src, value;
+};
+// Page src becomes page dst (src < 0: no page is copied); entry >= 0: that table entry becomes dst.
+struct CacheMove {
+    int32_t src, dst, entry;
+};
+// One entry of aif_cache_attend.
+struct CacheAsk {
+    const char *q;
+    char *out;
+    float *lse;
+    const int32_t *pos;
+    int64_t q_stride, out_stride;   // bytes
+    int32_t n_q, len, sinks, window, entry, pad_;
+};
+
+// Descriptors of a launch.  Few of them travel in the kernel's arguments (which hold 4 KB), more are uploaded.
+constexpr int CACHE_FEW_BYTES = 3456;
+struct CacheFew {
+    uint32_t w[CACHE_FEW_BYTES / 4];
+};
+struct CacheFar {
+    const char *dev;
+};
+struct CacheList {
+    const void *host;           // as they are on the host
+    const char *dev;            // where they are on the device, or null: in the arguments
+    int32_t n;
+    size_t bytes;
+};
+
+hipError_t launch_cache_append(const CacheShape &c, const CacheList &units, hipStream_t s);
+hipError_t launch_cache_read(const CacheShape &c, const CacheList &units, hipStream_t s);
+hipError_t launch_cache_fill(const CacheShape &c, const CacheList &fills, int longest, hipStream_t s);
+hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStream_t s);
+// asks: n CacheAsk, then n + 1 running numbers of rows (int32)
+hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, int64_t rows, hipStream_t s);
+
+// A descriptor in a kernel whose first argument holds or names them.
+template <class T> __device__ __forceinline__ T cache_desc(const CacheFew &, size_t off) { return arg_copy(kernel_arg<T>(off)); }
+template <class T> __device__ __forceinline__ T cache_desc(const CacheFar &far, size_t off) { return *(const T *)(as_global(far.dev) + off); }
+
+template <class F> hipError_t cache_launch(const CacheList &list, F &&go)
+{
+    if (list.dev) {
+        go(CacheFar{list.dev});
+    } else {
+        CacheFew few;
+        __builtin_memcpy(few.w, list.host, list.bytes);
+        go(few);
+    }
+    return hipGetLastError();
+}
+
+}  // namespace aif
