@@ -19,6 +19,8 @@ using namespace aif;
 namespace {
 constexpr int CACHE_NSLOT = 8;
 constexpr size_t CACHE_SLOT_BYTES = 64 << 10;
+constexpr int MIN_TILES = 8, MAX_SPLITS = 128;
+constexpr int BLOCKS_PER_CU = 4;            // of the attention kernels, about
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
 }  // namespace
@@ -28,6 +30,8 @@ struct aif_cache_ctx {
     aif_cache_config cfg{};
     int device = 0;
     CacheBook book;
+    int64_t max_parts = 0;                  // partial results that a call may leave
+    float *part = nullptr;
     std::vector<uint32_t> stamp;            // sequences that a call has named
     uint32_t stamp_now = 0;
     char *h_stage = nullptr, *h_stage_dev = nullptr;
@@ -41,6 +45,8 @@ struct aif_cache_ctx {
 };
 
 namespace {
+
+size_t attend_bytes(size_t n) { return n * sizeof(CacheAsk) + 2 * (n + 1) * sizeof(int32_t); }
 
 aif_status cfail(aif_cache_ctx *c, aif_status st, const char *fmt, ...)
 {
@@ -179,6 +185,7 @@ void cdestroy(aif_cache_ctx *c)
 {
     if (!c) return;
     if (c->shape.table) (void)hipFree(c->shape.table);
+    if (c->part) (void)hipFree(c->part);
     if (c->d_stage) (void)hipFree(c->d_stage);
     if (c->h_stage) (void)hipHostFree(c->h_stage);
     for (int i = 0; i < CACHE_NSLOT; ++i)
@@ -215,7 +222,12 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     CACHE_TRY(nullptr, hipGetDevice(&c->device));
     CACHE_TRY(nullptr, hipMalloc((void **)&s.table, (size_t)entries * sizeof(int32_t)));
     // a list of asks is one upload, whatever its length
-    const size_t asks = (size_t)f->max_requests * (sizeof(CacheAsk) + sizeof(int32_t)) + 64;
+    const size_t asks = attend_bytes(f->max_requests);
+    int n_cu = 0;
+    CACHE_TRY(nullptr, hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device));
+    // keys are split into keys / chunk parts, rounded down, and chunk is at least work / max_parts: no call leaves more
+    c->max_parts = (int64_t)BLOCKS_PER_CU * (n_cu > 0 ? n_cu : 256);
+    CACHE_TRY(nullptr, hipMalloc((void **)&c->part, (size_t)c->max_parts * cache_part_floats(32, s.dp) * sizeof(float)));
     c->slot_bytes = ((asks > CACHE_SLOT_BYTES ? asks : CACHE_SLOT_BYTES) + 255) / 256 * 256;
     CACHE_TRY(nullptr, staging_alloc(c->slot_bytes * CACHE_NSLOT, &c->h_stage, &c->h_stage_dev));
     CACHE_TRY(nullptr, hipMalloc((void **)&c->d_stage, c->slot_bytes * CACHE_NSLOT));
@@ -349,6 +361,46 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
     return batch.send(go);
 }
 
+// How a call's work is cut.  Rows go in tiles of 16 or 32 (fp32: 16, a query's three pieces take the registers); where the
+// (row tile, kv head) pairs are fewer than the device holds blocks, their keys are shared out as well, in splits of at least
+// MIN_TILES tiles of 32 keys, so that a split outlasts its start.
+static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *first, CachePlan &plan)
+{
+    const CacheShape &sh = c->shape;
+    int32_t *joins = first + n + 1;
+    int64_t most_rows = 0, work = 0;
+    for (int r = 0; r < n; ++r) most_rows = std::max(most_rows, (int64_t)asks[r].n_q * sh.group);
+    const int rows = plan.rows_of_tile = sh.dtype == 0 || most_rows <= 16 ? 16 : 32;
+    auto tiles_of = [&](const CacheAsk &a) { return ((int64_t)a.n_q * sh.group + rows - 1) / rows; };
+    auto keys_of = [&](const CacheAsk &a) {         // tiles of keys that a row tile sees, about
+        int64_t keys = a.len;
+        if (a.window && (!a.pos || a.n_q == 1)) keys = std::min<int64_t>(a.len, (int64_t)a.window + std::min(a.sinks, a.len));
+        return (keys + CACHE_TILE - 1) / CACHE_TILE;
+    };
+    for (int r = 0; r < n; ++r) work += tiles_of(asks[r]) * keys_of(asks[r]) * sh.n_kv;
+    const int64_t chunk = std::max<int64_t>(MIN_TILES, (work + c->max_parts - 1) / c->max_parts);
+    int64_t units = 0, joined = 0, parts = 0;
+    for (int r = 0; r < n; ++r) {
+        CacheAsk &a = asks[r];
+        first[r] = (int32_t)units;
+        joins[r] = (int32_t)joined;
+        const int64_t tiles = tiles_of(a);
+        a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, keys_of(a) / chunk), MAX_SPLITS);
+        a.part = (int32_t)parts;
+        units += tiles * a.splits;
+        if (a.splits > 1) {
+            joined += (int64_t)a.n_q * sh.group;
+            parts += tiles * a.splits * sh.n_kv;
+        }
+    }
+    first[n] = (int32_t)units;
+    joins[n] = (int32_t)joined;
+    plan.units = (int32_t)units;
+    plan.joins = (int32_t)joined;
+    plan.part = c->part;
+    return units <= INT32_MAX;
+}
+
 aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, int32_t n, void *hip_stream)
 {
     if (!c) return AIF_EINVAL;
@@ -372,7 +424,7 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
     if ((st = check_stream(c, s)) != AIF_OK) return st;
     if (rows == 0) return AIF_OK;
 
-    const size_t bytes = (size_t)n * sizeof(CacheAsk) + ((size_t)n + 1) * sizeof(int32_t);
+    const size_t bytes = attend_bytes((size_t)n);
     const bool far = bytes > CACHE_FEW_BYTES;
     int slot = 0;
     char *h = c->few;
@@ -384,23 +436,20 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
         h = c->h_stage + (size_t)slot * c->slot_bytes;
     }
     CacheAsk *ha = (CacheAsk *)h;
-    int32_t *first = (int32_t *)(h + (size_t)n * sizeof(CacheAsk));
-    int32_t at = 0;
     for (int r = 0; r < n; ++r) {
         const aif_cache_attend_req &q = reqs[r];
-        first[r] = at;
-        at += q.n_q;
         ha[r] = CacheAsk{(const char *)q.q, (char *)q.out, q.lse_out, q.positions, (q.q_stride ? q.q_stride : width) * esz,
-                         (q.out_stride ? q.out_stride : width) * esz, q.n_q, c->book.len(q.seq), q.sinks, q.window, c->book.entry(q.seq, 0), 0};
+                         (q.out_stride ? q.out_stride : width) * esz, q.n_q, c->book.len(q.seq), q.sinks, q.window, c->book.entry(q.seq, 0), 1, 0, 0};
     }
-    first[n] = at;
+    CachePlan plan{};
+    if (!plan_attend(c, ha, n, (int32_t *)(ha + n), plan)) return cfail(c, AIF_ERANGE, "one call has too many queries");
     CacheList l{h, nullptr, n, bytes};
     if (far) {
         const size_t off = (size_t)slot * c->slot_bytes;
         CACHE_TRY(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
         l.dev = c->d_stage + off;
     }
-    CACHE_TRY(c, launch_cache_attend(c->shape, l, rows, s));
+    CACHE_TRY(c, launch_cache_attend(c->shape, l, plan, s));
     if (far) {
         CACHE_TRY(c, hipEventRecord(c->ev[slot], s));
         c->ev_live[slot] = true;

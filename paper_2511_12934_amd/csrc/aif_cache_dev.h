@@ -47,7 +47,10 @@ struct CacheAsk {
     float *lse;
     const int32_t *pos;
     int64_t q_stride, out_stride;   // bytes
-    int32_t n_q, len, sinks, window, entry, pad_;
+    int32_t n_q, len, sinks, window, entry;
+    int32_t splits;             // blocks that share a row tile's keys
+    int32_t part;               // splits > 1: the first of its partial results
+    int32_t pad_;
 };
 
 // Descriptors of a launch.  Few of them travel in the kernel's arguments (which hold 4 KB), more are uploaded.
@@ -69,8 +72,18 @@ hipError_t launch_cache_append(const CacheShape &c, const CacheList &units, hipS
 hipError_t launch_cache_read(const CacheShape &c, const CacheList &units, hipStream_t s);
 hipError_t launch_cache_fill(const CacheShape &c, const CacheList &fills, int longest, hipStream_t s);
 hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStream_t s);
-// asks: n CacheAsk, then n + 1 running numbers of rows (int32)
-hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, int64_t rows, hipStream_t s);
+
+// Attention.  A row is a query and one of the `group` heads that share a kv head; a unit is a tile of rows and one of the splits of
+// its keys.  asks: n CacheAsk, then int32 first[n + 1], running numbers of units, then int32 joins[n + 1], running numbers of the
+// rows of the asks with splits > 1.  part: room for the results of their units (CachePart).
+struct CachePlan {
+    int32_t units, joins;       // of all asks
+    int32_t rows_of_tile;
+    float *part;
+};
+// A partial result: [rows][dp] sums, then [rows] maxima and [rows] sums of weights, fp32
+__host__ __device__ inline size_t cache_part_floats(int rows, int dp) { return (size_t)rows * (dp + 2); }
+hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const CachePlan &plan, hipStream_t s);
 
 // A descriptor in a kernel whose first argument holds or names them.
 template <class T> __device__ __forceinline__ T cache_desc(const CacheFew &, size_t off) { return arg_copy(kernel_arg<T>(off)); }

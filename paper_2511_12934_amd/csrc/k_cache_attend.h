@@ -1,0 +1,151 @@
+// What the user cache's attention kernels share: entries and blocks, who sees what, the tiles of 32 keys that a block walks, and
+// four-bit codes on their way to the matrix cores.
+#pragma once
+#include "aif_cache_dev.h"
+
+namespace aif {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
+
+// The blocks of a launch: running numbers of units behind the asks.  A unit is (row tile, split), tiles first.
+struct CacheGrid {
+    int32_t n, firsts;          // asks; byte offset of int32 first[n + 1]
+};
+
+__device__ __forceinline__ CacheAsk ask_at(const char *dev, int r)
+{
+    const size_t off = (size_t)r * sizeof(CacheAsk);
+    return dev ? *(const CacheAsk *)(as_global(dev) + off) : arg_copy(kernel_arg<CacheAsk>(off));
+}
+__device__ __forceinline__ int first_at(const char *dev, const CacheGrid &g, int i)
+{
+    const size_t off = (size_t)g.firsts + 4 * (size_t)i;
+    return dev ? *(const int32_t *)(as_global(dev) + off) : *kernel_arg<int32_t>(off);
+}
+// The ask that a unit belongs to: 64 running numbers at a time.
+__device__ __forceinline__ int ask_of(const char *dev, const CacheGrid &g, int unit, int lane)
+{
+    int r = 0;
+    for (int base = 1; base <= g.n; base += 64) {
+        const int i = base + lane;
+        const int f = first_at(dev, g, i <= g.n ? i : g.n);
+        const int below = __popcll(__ballot(i <= g.n && f <= unit));
+        r += below;
+        if (below < 64) break;
+    }
+    return __builtin_amdgcn_readfirstlane(r);
+}
+
+// What a row (query i and a head) sees: keys j <= last, and of those beyond `from` or before `sinks` only.
+struct Sight {
+    int last, from, sinks;
+    __device__ __forceinline__ bool sees(int j) const { return j <= last && (j >= from || j < sinks); }
+};
+__device__ __forceinline__ Sight sight_of(const CacheAsk &a, int i, bool is_row)
+{
+    int p = a.len - 1;
+    if (a.pos && is_row) p = a.pos[i];
+    p = is_row && p > -1 ? p : -1;
+    Sight s;
+    s.last = p < a.len - 1 ? p : a.len - 1;
+    s.from = a.window ? p - a.window + 1 : 0;       // p >= -1, window > 0: no overflow
+    s.sinks = a.window ? a.sinks : 0;
+    return s;
+}
+
+// The tiles of 32 keys that some row of a block sees: [0, head) and [body, end).  all_from, all_to: keys that every row of it sees.
+struct Walk {
+    int head, body, end;
+    int all_last, all_from, sinks;
+    __device__ __forceinline__ int count() const { return head + (end > body ? end - body : 0); }
+    __device__ __forceinline__ int tile(int t) const { return t < head ? t : t - head + body; }
+    __device__ __forceinline__ bool whole(int tile) const
+    {
+        const int j = tile * CACHE_TILE;
+        return j + CACHE_TILE - 1 <= all_last && (j >= all_from || j + CACHE_TILE <= sinks);
+    }
+};
+// min / max over the rows that see anything at all (last >= 0); lo_*: the smallest, hi_*: the largest
+__device__ __forceinline__ Walk walk_of(const CacheAsk &a, int lo_last, int hi_last, int lo_from, int hi_from)
+{
+    Walk w;
+    w.sinks = a.window ? a.sinks : 0;
+    w.all_last = lo_last;
+    w.all_from = hi_from;
+    w.end = (hi_last + CACHE_TILE) / CACHE_TILE;            // hi_last = -1: none
+    w.body = (lo_from > 0 ? lo_from : 0) / CACHE_TILE;
+    const int s = w.sinks < hi_last + 1 ? w.sinks : hi_last + 1;
+    const int head = (s + CACHE_TILE - 1) / CACHE_TILE;
+    w.body = w.body < w.end ? w.body : w.end;
+    w.head = head < w.body ? head : w.body;
+    return w;
+}
+
+// Eight codes as bf16, times 2^(byte - 127) (a byte of 255 gives NaN).
+__device__ __forceinline__ bf16x8 decode8(uint32_t codes, float scale)
+{
+    union {
+        bf16x2 h[4];
+        bf16x8 all;
+    } u;
+    u.h[0] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
+    u.h[1] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
+    u.h[2] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
+    u.h[3] = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
+    return u.all;
+}
+__device__ __forceinline__ float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Eight fp32 numbers as NP bf16 pieces: rounded once (NP = 1), or cut after 8, 16 and 24 bits, whose sum is the number (NP = 3).
+template <int NP> __device__ __forceinline__ void pieces8(const float *x, bf16x8 *out)
+{
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        if constexpr (NP == 1) {
+            out[0][e] = (__bf16)x[e];
+        } else {
+            float r = x[e];
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const uint32_t h = __float_as_uint(r) & 0xffff0000u;
+                out[p][e] = __builtin_bit_cast(__bf16, (uint16_t)(h >> 16));
+                r -= __uint_as_float(h);
+            }
+        }
+    }
+}
+
+// Features [at, at + 8) of a query as NP pieces, zeros past its end; an infinity is its first piece alone.
+template <int DT, int NP> __device__ __forceinline__ void query8(const char *q, int at, int d, bool live, bf16x8 *out)
+{
+    if constexpr (DT == 1) {
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (live && at < d) v = *(const uint4 *)(q + 2 * at);
+        out[0] = __builtin_bit_cast(bf16x8, v);
+    } else {
+        float x[8];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (live && at + 4 * h < d) v = *(const float4 *)(q + 4 * (at + 4 * h));
+            x[4 * h] = v.x, x[4 * h + 1] = v.y, x[4 * h + 2] = v.z, x[4 * h + 3] = v.w;
+        }
+        pieces8<NP>(x, out);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (__builtin_isinf(x[e])) out[1][e] = out[2][e] = (__bf16)0.f;
+    }
+}
+
+// Which query and query head row `row` of a kv head is, and where its features lie.
+struct RowOf {
+    int i, head;
+};
+__device__ __forceinline__ RowOf row_of(const CacheShape &c, int kvh, int row) { return RowOf{row / c.group, kvh * c.group + row % c.group}; }
+
+}  // namespace aif

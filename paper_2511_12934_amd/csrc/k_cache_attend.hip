@@ -1,107 +1,389 @@
 // Attention over sequences held in 4 bits (include/aif_cache.h: aif_cache_attend).
 //
-// One wave to a query row and head: 64 keys at a time, a lane to a key for the scores (the row's features from LDS), a lane
-// to four features for the values.  One pass over the sequence with a running maximum m and sum l:
-//   m' = max(m, s),  l' = l 2^(m - m') + sum 2^(s - m'),  o' = o 2^(m - m') + sum 2^(s - m') v,   s = score log2 e
-#include "aif_cache_dev.h"
+// One pass over a sequence with a running maximum m and sum l of a row's weights, in powers of two:
+//   s = scale log2 e <q, k>,  m' = max(m, s),  l' = l 2^(m - m') + sum 2^(s - m'),  o' = o 2^(m - m') + sum 2^(s - m') v
+// and o / l at the end.  Any reference in the place of m gives the same quotient, so m only follows a maximum that has grown by
+// more than 2^8 beyond it: the weights stay below 2^8, and nearly every tile goes without a reduction across lanes.
+//
+// k_cache_few.  What bounds it is the cache itself, 34 dp bytes per kv head and 32 keys, read once.  A wave takes 32 keys at a
+// time.  Codes go from memory to registers to bf16 (exact: v_cvt_scalef32_pk_bf16_fp4, two codes an instruction) and on to
+// the 16x16x32 products: S^T = K Q^T (a lane's codes of a key are the k-slots; which features stand in which slot is free, so a
+// lane takes dp / 4 neighbouring ones), whose result leaves a lane with eight keys of ONE row: the weights are the second
+// product's operand where they are, O^T = V^T P^T.  V has to be turned, features to rows: bf16 rows of 32 keys in the wave's own LDS,
+// read back by ds_read_b64_tr_b16 (four keys of one feature a lane); rows are 32 bytes longer than their features, so that
+// eight rows' pieces lie in different banks.  No barrier in the loop; the four waves of a block take the tiles in turn, each
+// with the next tile's codes already asked for, and join through LDS.
+#include "k_cache_attend.h"
 
 namespace aif {
 
 namespace {
 
-__device__ __forceinline__ float code_value(uint32_t c, float scale)
+constexpr float LAZY = 8.f;             // how far, in powers of two, a score may pass the reference
+
+// What a lane holds of a tile: of key lane % 16 (+ 16) the features [lane / 16 * dp / 4, + dp / 4), NW words of eight.
+template <int NW> struct RawTile {
+    uint32_t k[2][NW], v[2][NW], ks[2], vs[2];      // ks, vs: up to four scale bytes, from the first block of the lane's features on
+};
+
+template <int NW> __device__ __forceinline__ void load_words(const char *p, uint32_t *w)
 {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    const bf16x2 v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, 0);
-    return __uint_as_float(__builtin_bit_cast(uint32_t, v) << 16);
+    if constexpr (NW % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < NW / 4; ++i) {
+            const uint4 x = ((const uint4 *)p)[i];
+            w[4 * i] = x.x, w[4 * i + 1] = x.y, w[4 * i + 2] = x.z, w[4 * i + 3] = x.w;
+        }
+    } else if constexpr (NW % 2 == 0) {
+#pragma unroll
+        for (int i = 0; i < NW / 2; ++i) {
+            const uint2 x = ((const uint2 *)p)[i];
+            w[2 * i] = x.x, w[2 * i + 1] = x.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NW; ++i) w[i] = ((const uint32_t *)p)[i];
+    }
 }
 
-template <int DT, class ARGS> __global__ __launch_bounds__(64) void k_cache_attend_row(ARGS list, CacheShape c, int n)
+// blocks that a lane's NW words can lie in
+template <int NW> constexpr int blocks_of() { return NW == 7 ? 3 : NW == 3 || NW > 4 ? 2 : 1; }
+
+template <int NW> __device__ __forceinline__ void load_tile(const char *tile, int lane, RawTile<NW> &r)
 {
-    __shared__ float qs[CACHE_MAX_DP];
-    const size_t firsts = (size_t)n * sizeof(CacheAsk);
-    const int lane = threadIdx.x, row = blockIdx.x, head = blockIdx.y;
-    int r = 0;
-    while (cache_desc<int32_t>(list, firsts + 4 * (size_t)(r + 1)) <= row) ++r;
-    const CacheAsk a = cache_desc<CacheAsk>(list, (size_t)r * sizeof(CacheAsk));
-    const int i = row - cache_desc<int32_t>(list, firsts + 4 * (size_t)r), esz = DT == 0 ? 4 : 2;
-    const char *q = a.q + (size_t)i * a.q_stride + (size_t)head * c.d_head * esz;
-    for (int f = lane; f < c.dp; f += 64) {
-        float x = 0.f;
-        if (f < c.d_head) x = DT == 0 ? ((const float *)q)[f] : bf2f(((const uint16_t *)q)[f]);
-        qs[f] = x;
+    constexpr int DP = 32 * NW;
+    const int key = lane & 15, grp = lane >> 4, lo = grp * NW / 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int row = 16 * h + key;
+        load_words<NW>(tile + row * (DP / 2) + grp * (DP / 8), r.k[h]);
+        load_words<NW>(tile + 16 * DP + row * (DP / 2) + grp * (DP / 8), r.v[h]);
+        const uint8_t *ks = (const uint8_t *)tile + 32 * DP + row * NW, *vs = ks + DP;
+        r.ks[h] = ks[lo], r.vs[h] = vs[lo];
+#pragma unroll
+        for (int b = 1; b < blocks_of<NW>(); ++b) {         // (the last group's last bytes may be the next row's: not used then)
+            const int at = lo + b < NW ? lo + b : NW - 1;
+            r.ks[h] |= (uint32_t)ks[at] << (8 * b);
+            r.vs[h] |= (uint32_t)vs[at] << (8 * b);
+        }
     }
-    __syncthreads();
-    int p = a.pos ? a.pos[i] : a.len - 1;
-    p = p < -1 ? -1 : p;
-    const float k2 = c.scale * 1.44269504088896340736f;
-    const size_t head_at = (size_t)(head / c.group) * cache_head_bytes(c);
-    float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    const int end = p < a.len - 1 ? p + 1 : a.len;
-    for (int base = 0; base < end; base += 64) {
-        const int j = base + lane;
-        bool see = j < end && (a.window == 0 || j > p - a.window || j < a.sinks);
-        int page = -1;
-        if (see) page = c.table[a.entry + j / c.page_len];
-        see = page >= 0;
-        const char *tile = c.pool + (size_t)(see ? page : 0) * c.page_bytes + head_at + (size_t)(j % c.page_len / CACHE_TILE) * cache_tile_bytes(c.dp);
-        const int jr = j % CACHE_TILE, nb = c.dp / 32;
-        float s = -INFINITY;
-        if (see) {
-            float sum = 0.f;
-            for (int b = 0; b < nb; ++b) {
-                const float scale = __uint_as_float((uint32_t)(uint8_t)tile[32 * c.dp + jr * nb + b] << 23);
-                for (int w = 0; w < 4; ++w) {
-                    const uint32_t codes = *(const uint32_t *)(tile + jr * (c.dp / 2) + 16 * b + 4 * w);
-                    for (int e = 0; e < 8; ++e) sum += qs[32 * b + 8 * w + e] * code_value(codes >> (4 * e), scale);
+}
+
+// the scale of word w of a lane's NW
+template <int NW> __device__ __forceinline__ float word_scale(uint32_t bytes, int grp, int w)
+{
+    if constexpr (blocks_of<NW>() == 1) return scale_of(bytes);
+    else if constexpr (NW == 8) return scale_of((bytes >> (w / 4 * 8)) & 255);
+    else return scale_of((bytes >> (((grp * NW + w) / 4 - grp * NW / 4) * 8)) & 255);
+}
+
+template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache_few(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
+{
+    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 16 * NT, FT = DP / 16;
+    constexpr int STRIDE = 2 * DP + 32, WAVE_BYTES = 32 * STRIDE;
+    static_assert(WAVE_BYTES >= 16 * DP * 4, "a wave's sums fit its room for values");
+    __shared__ __align__(16) char lds[4 * WAVE_BYTES];
+    __shared__ float ml[2][4][ROWS];
+    (void)few;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4, kvh = blockIdx.y;
+    const int r = ask_of(dev, g, blockIdx.x, lane);
+    const CacheAsk a = ask_at(dev, r);
+    const int unit = (int)blockIdx.x - first_at(dev, g, r), tile_of_rows = unit / a.splits, split = unit % a.splits;
+    const int n_rows = a.n_q * c.group, row0 = tile_of_rows * ROWS;
+
+    // the rows: who sees what, and their features
+    Sight see[NT];
+    bf16x8 q[NT][NP][NW];
+    int lo_last = INT32_MAX, hi_last = -1, lo_from = INT32_MAX, hi_from = -1;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        const int row = row0 + 16 * t + col;
+        const bool is_row = row < n_rows;
+        const RowOf o = row_of(c, kvh, is_row ? row : 0);
+        see[t] = sight_of(a, o.i, is_row);
+        if (is_row) {
+            lo_last = min(lo_last, see[t].last);
+            hi_last = max(hi_last, see[t].last);
+            hi_from = max(hi_from, see[t].from);
+            if (see[t].last >= 0) lo_from = min(lo_from, see[t].from);
+        }
+        const char *qr = a.q + (size_t)o.i * a.q_stride + (size_t)o.head * c.d_head * (DT == 0 ? 4 : 2);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            bf16x8 p[NP];
+            query8<DT, NP>(qr, grp * (DP / 4) + 8 * w, c.d_head, is_row, p);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) q[t][i][w] = p[i];
+        }
+    }
+#pragma unroll
+    for (int x = 1; x < 16; x *= 2) {
+        lo_last = min(lo_last, __shfl_xor(lo_last, x));
+        hi_last = max(hi_last, __shfl_xor(hi_last, x));
+        lo_from = min(lo_from, __shfl_xor(lo_from, x));
+        hi_from = max(hi_from, __shfl_xor(hi_from, x));
+    }
+    lo_last = __builtin_amdgcn_readfirstlane(lo_last);
+    hi_last = __builtin_amdgcn_readfirstlane(hi_last);
+    lo_from = __builtin_amdgcn_readfirstlane(lo_from);
+    hi_from = __builtin_amdgcn_readfirstlane(hi_from);
+    const Walk walk = walk_of(a, lo_last, hi_last, lo_from, hi_from);
+    const int64_t n_tiles = walk.count();
+    const int t_end = (int)(n_tiles * (split + 1) / a.splits);
+
+    const char *pool = c.pool + (size_t)kvh * cache_head_bytes(c);
+    const int tiles_per_page = c.page_len / CACHE_TILE;
+    // tile t of the walk, or null: it lies in a page that was dropped
+    auto address = [&](int t) -> const char * {
+        const int tile = walk.tile(t), page = c.table[a.entry + tile / tiles_per_page];
+        return page < 0 ? nullptr : pool + (size_t)page * c.page_bytes + (size_t)(tile % tiles_per_page) * cache_tile_bytes(DP);
+    };
+
+    f32x4 acc[NT][FT];
+    float m[NT], l[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        m[t] = -INFINITY, l[t] = 0.f;
+#pragma unroll
+        for (int f = 0; f < FT; ++f) acc[t][f] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const float k2 = c.scale * LOG2E;
+    char *mine = lds + wave * WAVE_BYTES;
+    typedef s16x4 __attribute__((address_space(3))) *lds4_t;
+    const char *turned = mine + (4 * grp + col / 4) * STRIDE + col % 4 * 8;      // this lane's piece of four keys and 16 features
+
+    int t = (int)(n_tiles * split / a.splits) + wave;
+    RawTile<NW> raw;
+    const char *at = t < t_end ? address(t) : nullptr;
+    if (at) load_tile<NW>(at, lane, raw);
+    for (; t < t_end; t += 4) {
+        const RawTile<NW> now = raw;
+        const bool here = at != nullptr;
+        at = t + 4 < t_end ? address(t + 4) : nullptr;
+        if (at) load_tile<NW>(at, lane, raw);
+        if (!here) continue;
+        const int tile = walk.tile(t), j0 = tile * CACHE_TILE + 4 * grp;
+
+        // values: as bf16 rows of the wave's LDS.  A block that is not finite -- NaN, or bytes that nobody wrote -- becomes zeros:
+        // who sees it gets NaN below.
+        uint32_t odd = 0;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float sc = word_scale<NW>(now.vs[h], grp, w);
+                const bool fine = sc < 0x1p126f;
+                odd |= fine || tile * CACHE_TILE + 16 * h + col > hi_last ? 0u : 1u;
+                *(bf16x8 *)(mine + (16 * h + col) * STRIDE + (grp * (DP / 4) + 8 * w) * 2) = decode8(fine ? now.v[h][w] : 0u, fine ? sc : 1.f);
+            }
+        }
+
+        // scores
+        f32x4 s[NT][2];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) s[i][0] = s[i][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const bf16x8 k = decode8(now.k[h][w], word_scale<NW>(now.ks[h], grp, w));
+#pragma unroll
+                for (int i = 0; i < NT; ++i)
+#pragma unroll
+                    for (int p = NP - 1; p >= 0; --p) s[i][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i][p][w], s[i][h], 0, 0, 0);
+            }
+
+        const bool whole = walk.whole(tile);
+        bf16x8 weights[NT][NP];
+#pragma unroll
+        for (int i = 0; i < NT; ++i) {
+            float x[8], top = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = s[i][e / 4][e % 4] * k2;
+            if (!whole) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = see[i].sees(j0 + 16 * (e / 4) + e % 4) ? x[e] : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) top = fmaxf(top, x[e]);
+            if (__ballot(top > m[i] + LAZY)) {
+                top = fmaxf(top, __shfl_xor(top, 16));
+                top = fmaxf(top, __shfl_xor(top, 32));
+                const float m2 = fmaxf(m[i], top), back = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - m2);
+                m[i] = m2;
+                l[i] *= back;
+#pragma unroll
+                for (int f = 0; f < FT; ++f) acc[i][f] *= back;
+            }
+            const float ref = m[i] == -INFINITY ? 0.f : m[i];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
+                l[i] += x[e];
+            }
+            pieces8<NP>(x, weights[i]);
+        }
+
+#pragma unroll
+        for (int f = 0; f < FT; ++f) {
+            union {
+                s16x4 h[2];
+                bf16x8 all;
+            } v;
+            v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turned + f * 32));
+            v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turned + 16 * STRIDE + f * 32));
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) acc[i][f] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.all, weights[i][p], acc[i][f], 0, 0, 0);
+        }
+
+        if (__ballot(odd)) {
+            // a row that sees a block of values that is not finite: its 32 features are NaN
+            for (int key = 0; key < CACHE_TILE; ++key) {
+                const int from = key & 15;
+                uint32_t bytes[4];
+                #pragma unroll
+                for (int gr = 0; gr < 4; ++gr) bytes[gr] = __shfl(key < 16 ? now.vs[0] : now.vs[1], from + 16 * gr);
+#pragma unroll
+                for (int f = 0; f < FT; ++f) {              // 16 features of block f / 2, which group f / 2 * 4 / NW holds
+                    const int gr = f / 2 * 4 / NW, lo = gr * NW / 4;
+                    const float sc = scale_of((bytes[gr] >> ((f / 2 - lo) * 8)) & 255);
+                    if (sc < 0x1p126f) continue;
+#pragma unroll
+                    for (int i = 0; i < NT; ++i)
+                        if (see[i].sees(tile * CACHE_TILE + key)) acc[i][f] += __builtin_nanf("");
                 }
             }
-            s = sum * k2;
         }
-        float most = s;
-        for (int d = 1; d < 64; d *= 2) most = fmaxf(most, __shfl_xor(most, d));
-        const float m2 = fmaxf(m, most), ref = m2 == -INFINITY ? 0.f : m2;
-        const float w = see ? __builtin_amdgcn_exp2f(s - ref) : 0.f, back = __builtin_amdgcn_exp2f(m - ref);
-        m = m2;
-        float sum = w;
-        for (int d = 1; d < 64; d *= 2) sum += __shfl_xor(sum, d);
-        l = l * back + sum;
-        for (int f = 0; f < 4; ++f) o[f] *= back;
-        unsigned long long seen = __ballot(see);
-        while (seen) {
-            const int t = __ffsll(seen) - 1;
-            seen &= seen - 1;
-            const float wt = __shfl(w, t);
-            const char *vt = (const char *)(((unsigned long long)(uint32_t)__shfl((int)((uintptr_t)tile >> 32), t) << 32) | (uint32_t)__shfl((int)(uintptr_t)tile, t));
-            const int vr = (base + t) % CACHE_TILE;
-            if (4 * lane < c.dp) {
-                const uint32_t codes = *(const uint16_t *)(vt + 16 * c.dp + vr * (c.dp / 2) + 2 * lane);
-                const float scale = __uint_as_float((uint32_t)(uint8_t)vt[33 * c.dp + vr * nb + lane / 8] << 23);
-                for (int f = 0; f < 4; ++f) o[f] += wt * code_value(codes >> (4 * f), scale);
+    }
+
+    // the four waves' parts become one: a common reference, then sums through LDS
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        l[i] += __shfl_xor(l[i], 16);
+        l[i] += __shfl_xor(l[i], 32);
+        if (grp == 0) ml[0][wave][16 * i + col] = m[i], ml[1][wave][16 * i + col] = l[i];
+    }
+    __syncthreads();
+    const int esz = DT == 0 ? 4 : 2;
+    float *pt = part + ((size_t)a.part + (size_t)kvh * ((n_rows + ROWS - 1) / ROWS) * a.splits + unit) * cache_part_floats(ROWS, DP);    // (splits > 1)
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {
+        float top = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][16 * i + col]);
+        const float back = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - top);
+        float *sums = (float *)mine;            // [16 rows][DP]
+        if (i) __syncthreads();
+#pragma unroll
+        for (int f = 0; f < FT; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[col * DP + 16 * f + 4 * grp + e] = m[i] == -INFINITY ? acc[i][f][e] * 0.f : acc[i][f][e] * back;
+        __syncthreads();
+        for (int x = threadIdx.x; x < 16 * DP; x += 256) {
+            const int cl = x / DP, f = x % DP, row = row0 + 16 * i + cl;
+            float mt = -INFINITY, sum = 0.f, o = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) mt = fmaxf(mt, ml[0][w][16 * i + cl]);
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                o += ((const float *)(lds + w * WAVE_BYTES))[x];
+                const float mw = ml[0][w][16 * i + cl];
+                sum += mw == -INFINITY ? ml[1][w][16 * i + cl] : ml[1][w][16 * i + cl] * __builtin_amdgcn_exp2f(mw - mt);
+            }
+            if (a.splits > 1) {
+                pt[(16 * i + cl) * DP + f] = o;
+                if (f == 0) pt[ROWS * DP + 16 * i + cl] = mt, pt[ROWS * DP + ROWS + 16 * i + cl] = sum;
+            } else if (row < n_rows) {
+                const RowOf at_row = row_of(c, kvh, row);
+                const float v = sum == 0.f ? 0.f : o / sum;
+                if (f < c.d_head) {
+                    char *out = a.out + (size_t)at_row.i * a.out_stride + ((size_t)at_row.head * c.d_head + f) * esz;
+                    if (DT == 0) *(float *)out = v;
+                    else *(uint16_t *)out = f2bf(v);
+                }
+                if (f == 0 && a.lse) a.lse[(size_t)at_row.i * c.n_heads + at_row.head] = sum == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(sum)) * LN2;
             }
         }
     }
-    char *out = a.out + (size_t)i * a.out_stride + (size_t)head * c.d_head * esz;
-    for (int f = 0; f < 4; ++f)
-        if (4 * lane + f < c.d_head) {
-            const float v = l == 0.f ? 0.f : o[f] / l;
-            if (DT == 0) ((float *)out)[4 * lane + f] = v;
-            else ((uint16_t *)out)[4 * lane + f] = f2bf(v);
+}
+
+// Rows whose keys several blocks shared: their parts, in the order of the keys.  A block to a row and kv head.
+template <int DT> __global__ __launch_bounds__(128) void k_cache_join(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, const float *part, int rows_of_tile)
+{
+    (void)few;
+    const int lane = threadIdx.x & 63, kvh = blockIdx.y;
+    const int r = ask_of(dev, g, blockIdx.x, lane);
+    const CacheAsk a = ask_at(dev, r);
+    const int row = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group, tiles = (n_rows + rows_of_tile - 1) / rows_of_tile;
+    const size_t each = cache_part_floats(rows_of_tile, c.dp);
+    const float *p = part + ((size_t)a.part + ((size_t)kvh * tiles + row / rows_of_tile) * a.splits) * each;
+    const int cl = row % rows_of_tile;
+    const float *ms = p + (size_t)rows_of_tile * c.dp + cl, *ls = ms + rows_of_tile;
+    float mt = -INFINITY;
+    for (int s = lane; s < a.splits; s += 64) mt = fmaxf(mt, ms[s * each]);
+    for (int x = 1; x < 64; x *= 2) mt = fmaxf(mt, __shfl_xor(mt, x));
+    const RowOf at = row_of(c, kvh, row);
+    float sum = 0.f, o[2] = {0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float mw = ms[s * each], back = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw - mt);     // without a maximum: zeros, or NaN
+        sum += ls[s * each] * back;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int f = threadIdx.x + 128 * h;
+            if (f < c.dp) o[h] += p[s * each + (size_t)cl * c.dp + f] * back;
         }
-    if (a.lse && lane == 0) a.lse[(size_t)i * c.n_heads + head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994530942f;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int f = threadIdx.x + 128 * h;
+        if (f >= c.d_head) continue;
+        const float v = sum == 0.f ? 0.f : o[h] / sum;
+        char *out = a.out + (size_t)at.i * a.out_stride + ((size_t)at.head * c.d_head + f) * (DT == 0 ? 4 : 2);
+        if (DT == 0) *(float *)out = v;
+        else *(uint16_t *)out = f2bf(v);
+    }
+    if (threadIdx.x == 0 && a.lse) a.lse[(size_t)at.i * c.n_heads + at.head] = sum == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(sum)) * LN2;
 }
 
 }  // namespace
 
-hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, int64_t rows, hipStream_t s)
+namespace {
+template <int DT, int NW, int NT> void few(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePlan &p, hipStream_t s)
 {
-    if (rows == 0) return hipSuccess;
-    return cache_launch(asks, [&](auto args) {
-        using A = decltype(args);
-        const dim3 grid((unsigned)rows, c.n_heads);
-        if (c.dtype == 0) hipLaunchKernelGGL((k_cache_attend_row<0, A>), grid, dim3(64), 0, s, args, c, asks.n);
-        else hipLaunchKernelGGL((k_cache_attend_row<1, A>), grid, dim3(64), 0, s, args, c, asks.n);
-    });
+    hipLaunchKernelGGL((k_cache_few<DT, NW, NT>), dim3(p.units, c.n_kv), dim3(256), 0, s, args, dev, g, c, p.part);
+}
+template <int NW> void few_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePlan &p, hipStream_t s)
+{
+    if (c.dtype == 0) few<0, NW, 1>(args, dev, g, c, p, s);
+    else if (p.rows_of_tile == 16) few<1, NW, 1>(args, dev, g, c, p, s);
+    else few<1, NW, 2>(args, dev, g, c, p, s);
+}
+}  // namespace
+
+hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const CachePlan &p, hipStream_t s)
+{
+    if (p.units == 0) return hipSuccess;
+    CacheFew args;
+    if (!asks.dev) __builtin_memcpy(args.w, asks.host, asks.bytes);
+    CacheGrid g{asks.n, (int32_t)(asks.n * sizeof(CacheAsk))};
+    switch (c.dp / 32) {
+    case 1: few_of<1>(args, asks.dev, g, c, p, s); break;
+    case 2: few_of<2>(args, asks.dev, g, c, p, s); break;
+    case 3: few_of<3>(args, asks.dev, g, c, p, s); break;
+    case 4: few_of<4>(args, asks.dev, g, c, p, s); break;
+    case 5: few_of<5>(args, asks.dev, g, c, p, s); break;
+    case 6: few_of<6>(args, asks.dev, g, c, p, s); break;
+    case 7: few_of<7>(args, asks.dev, g, c, p, s); break;
+    default: few_of<8>(args, asks.dev, g, c, p, s); break;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.joins == 0) return e;
+    g.firsts += 4 * (asks.n + 1);
+    if (c.dtype == 0) hipLaunchKernelGGL(k_cache_join<0>, dim3(p.joins, c.n_kv), dim3(128), 0, s, args, asks.dev, g, c, p.part, p.rows_of_tile);
+    else hipLaunchKernelGGL(k_cache_join<1>, dim3(p.joins, c.n_kv), dim3(128), 0, s, args, asks.dev, g, c, p.part, p.rows_of_tile);
+    return hipGetLastError();
 }
 
 }  // namespace aif
