@@ -19,8 +19,7 @@ using namespace aif;
 namespace {
 constexpr int CACHE_NSLOT = 8;
 constexpr size_t CACHE_SLOT_BYTES = 64 << 10;
-constexpr int MIN_TILES = 8, MAX_SPLITS = 128;
-constexpr int BLOCKS_PER_CU = 4;            // of the attention kernels, about
+constexpr int FEW_ROWS = 64, MIN_TILES = 8, MAX_SPLITS = 128, PART_ROWS = 256;     // plan_attend
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
 }  // namespace
@@ -30,8 +29,8 @@ struct aif_cache_ctx {
     aif_cache_config cfg{};
     int device = 0;
     CacheBook book;
-    int64_t max_parts = 0;                  // partial results that a call may leave
-    float *part = nullptr;
+    int n_cu = 256;
+    float *part[2] = {};                    // partial results of the attention kernels for few and for many rows
     std::vector<uint32_t> stamp;            // sequences that a call has named
     uint32_t stamp_now = 0;
     char *h_stage = nullptr, *h_stage_dev = nullptr;
@@ -46,7 +45,7 @@ struct aif_cache_ctx {
 
 namespace {
 
-size_t attend_bytes(size_t n) { return n * sizeof(CacheAsk) + 2 * (n + 1) * sizeof(int32_t); }
+size_t attend_bytes(size_t n) { return n * sizeof(CacheAsk) + 4 * (n + 1) * sizeof(int32_t); }
 
 aif_status cfail(aif_cache_ctx *c, aif_status st, const char *fmt, ...)
 {
@@ -185,7 +184,8 @@ void cdestroy(aif_cache_ctx *c)
 {
     if (!c) return;
     if (c->shape.table) (void)hipFree(c->shape.table);
-    if (c->part) (void)hipFree(c->part);
+    for (float *p : c->part)
+        if (p) (void)hipFree(p);
     if (c->d_stage) (void)hipFree(c->d_stage);
     if (c->h_stage) (void)hipHostFree(c->h_stage);
     for (int i = 0; i < CACHE_NSLOT; ++i)
@@ -200,7 +200,7 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     if (f->n_pages <= 0 || f->max_seqs <= 0 || f->max_len <= 0 || f->max_requests <= 0 || f->max_queries <= 0)
         return cfail(nullptr, AIF_EINVAL, "non-positive size in aif_cache_config");
     if (f->max_requests > 65535) return cfail(nullptr, AIF_ESHAPE, "max_requests %d is above 65535", f->max_requests);
-    if (!(f->scale == f->scale) || f->scale - f->scale != 0.f) return cfail(nullptr, AIF_EINVAL, "scale is not finite");
+    if (!(f->scale >= 0.f) || f->scale - f->scale != 0.f) return cfail(nullptr, AIF_EINVAL, "scale is negative or not finite");
     if (!pool || (uintptr_t)pool % 64) return cfail(nullptr, AIF_EINVAL, "the pool is NULL or not 64-byte aligned");
     c->cfg = *f;
     CacheShape &s = c->shape;
@@ -225,9 +225,8 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     const size_t asks = attend_bytes(f->max_requests);
     int n_cu = 0;
     CACHE_TRY(nullptr, hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device));
-    // keys are split into keys / chunk parts, rounded down, and chunk is at least work / max_parts: no call leaves more
-    c->max_parts = (int64_t)BLOCKS_PER_CU * (n_cu > 0 ? n_cu : 256);
-    CACHE_TRY(nullptr, hipMalloc((void **)&c->part, (size_t)c->max_parts * cache_part_floats(32, s.dp) * sizeof(float)));
+    if (n_cu > 0) c->n_cu = n_cu;
+    for (float *&p : c->part) CACHE_TRY(nullptr, hipMalloc((void **)&p, cache_part_floats(c->n_cu * PART_ROWS, s.dp) * sizeof(float)));
     c->slot_bytes = ((asks > CACHE_SLOT_BYTES ? asks : CACHE_SLOT_BYTES) + 255) / 256 * 256;
     CACHE_TRY(nullptr, staging_alloc(c->slot_bytes * CACHE_NSLOT, &c->h_stage, &c->h_stage_dev));
     CACHE_TRY(nullptr, hipMalloc((void **)&c->d_stage, c->slot_bytes * CACHE_NSLOT));
@@ -361,44 +360,61 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
     return batch.send(go);
 }
 
-// How a call's work is cut.  Rows go in tiles of 16 or 32 (fp32: 16, a query's three pieces take the registers); where the
-// (row tile, kv head) pairs are fewer than the device holds blocks, their keys are shared out as well, in splits of at least
-// MIN_TILES tiles of 32 keys, so that a split outlasts its start.
-static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *first, CachePlan &plan)
+// How a call's work is cut.  Entries of up to FEW_ROWS rows (queries times heads of a kv head) go to the kernel whose row tiles are 16 or 32
+// (fp32: 16, a query's three pieces take the registers), the others to the one whose tiles are 128 or, bf16 heads of up to 128 and
+// enough of them, 256.  Where the (row tile, kv head) pairs are fewer than the device holds blocks, their keys are shared
+// out as well, in splits of at least MIN_TILES tiles of 32 keys, so that a split outlasts its start.  Partial results have room for
+// PART_ROWS rows a compute unit and kernel: tiles * splits <= tiles * keys / chunk <= work / chunk <= room.
+static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays, CachePlan &plan, size_t &bytes)
 {
     const CacheShape &sh = c->shape;
-    int32_t *joins = first + n + 1;
-    int64_t most_rows = 0, work = 0;
-    for (int r = 0; r < n; ++r) most_rows = std::max(most_rows, (int64_t)asks[r].n_q * sh.group);
-    const int rows = plan.rows_of_tile = sh.dtype == 0 || most_rows <= 16 ? 16 : 32;
-    auto tiles_of = [&](const CacheAsk &a) { return ((int64_t)a.n_q * sh.group + rows - 1) / rows; };
+    auto rows_of = [&](const CacheAsk &a) { return (int64_t)a.n_q * sh.group; };
     auto keys_of = [&](const CacheAsk &a) {         // tiles of keys that a row tile sees, about
         int64_t keys = a.len;
         if (a.window && (!a.pos || a.n_q == 1)) keys = std::min<int64_t>(a.len, (int64_t)a.window + std::min(a.sinks, a.len));
         return (keys + CACHE_TILE - 1) / CACHE_TILE;
     };
-    for (int r = 0; r < n; ++r) work += tiles_of(asks[r]) * keys_of(asks[r]) * sh.n_kv;
-    const int64_t chunk = std::max<int64_t>(MIN_TILES, (work + c->max_parts - 1) / c->max_parts);
-    int64_t units = 0, joined = 0, parts = 0;
-    for (int r = 0; r < n; ++r) {
-        CacheAsk &a = asks[r];
-        first[r] = (int32_t)units;
-        joins[r] = (int32_t)joined;
-        const int64_t tiles = tiles_of(a);
-        a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, keys_of(a) / chunk), MAX_SPLITS);
-        a.part = (int32_t)parts;
-        units += tiles * a.splits;
-        if (a.splits > 1) {
-            joined += (int64_t)a.n_q * sh.group;
-            parts += tiles * a.splits * sh.n_kv;
+    bytes = (size_t)n * sizeof(CacheAsk);
+    for (int kind = 0; kind < 2; ++kind) {
+        CachePart &p = kind ? plan.many : plan.few;
+        auto mine = [&](const CacheAsk &a) { return a.n_q > 0 && (rows_of(a) > FEW_ROWS) == (kind == 1); };
+        int64_t most = 0, wide = 0;
+        for (int r = 0; r < n; ++r)
+            if (mine(asks[r])) most = std::max(most, rows_of(asks[r])), wide += (rows_of(asks[r]) + 255) / 256 * sh.n_kv;
+        if (most == 0) continue;
+        const int rows = p.rows_of_tile = kind ? (sh.dtype == 1 && sh.dp <= 128 && wide >= 2 * c->n_cu ? 256 : 128) : (sh.dtype == 0 || most <= 16 ? 16 : 32);
+        const int64_t room = (int64_t)c->n_cu * PART_ROWS / rows;
+        auto tiles_of = [&](const CacheAsk &a) { return (rows_of(a) + rows - 1) / rows; };
+        int64_t work = 0, units = 0, joined = 0, parts = 0;
+        for (int r = 0; r < n; ++r)
+            if (mine(asks[r])) work += tiles_of(asks[r]) * keys_of(asks[r]) * sh.n_kv;
+        const int64_t blocks = std::min<int64_t>(room, (int64_t)c->n_cu * (kind ? 2 : 4));
+        const int64_t chunk = std::max<int64_t>(MIN_TILES, (work + blocks - 1) / blocks);
+        int32_t *first = arrays, *joins = arrays + n + 1;
+        arrays += 2 * (n + 1);
+        bytes += 2 * ((size_t)n + 1) * sizeof(int32_t);
+        for (int r = 0; r < n; ++r) {
+            CacheAsk &a = asks[r];
+            first[r] = (int32_t)units;
+            joins[r] = (int32_t)joined;
+            if (!mine(a)) continue;
+            const int64_t tiles = tiles_of(a);
+            a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, keys_of(a) / chunk), MAX_SPLITS);
+            a.part = (int32_t)parts;
+            units += tiles * a.splits;
+            if (a.splits > 1) {
+                joined += rows_of(a);
+                parts += tiles * a.splits * sh.n_kv;
+            }
+            if (units > INT32_MAX) return false;
         }
+        first[n] = (int32_t)units;
+        joins[n] = (int32_t)joined;
+        p.units = (int32_t)units;
+        p.joins = (int32_t)joined;
+        p.part = c->part[kind];
     }
-    first[n] = (int32_t)units;
-    joins[n] = (int32_t)joined;
-    plan.units = (int32_t)units;
-    plan.joins = (int32_t)joined;
-    plan.part = c->part;
-    return units <= INT32_MAX;
+    return true;
 }
 
 aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, int32_t n, void *hip_stream)
@@ -424,8 +440,8 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
     if ((st = check_stream(c, s)) != AIF_OK) return st;
     if (rows == 0) return AIF_OK;
 
-    const size_t bytes = attend_bytes((size_t)n);
-    const bool far = bytes > CACHE_FEW_BYTES;
+    const bool far = attend_bytes((size_t)n) > CACHE_FEW_BYTES;
+    size_t bytes = 0;
     int slot = 0;
     char *h = c->few;
     if (far) {
@@ -442,7 +458,7 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
                          (q.out_stride ? q.out_stride : width) * esz, q.n_q, c->book.len(q.seq), q.sinks, q.window, c->book.entry(q.seq, 0), 1, 0, 0};
     }
     CachePlan plan{};
-    if (!plan_attend(c, ha, n, (int32_t *)(ha + n), plan)) return cfail(c, AIF_ERANGE, "one call has too many queries");
+    if (!plan_attend(c, ha, n, (int32_t *)(ha + n), plan, bytes)) return cfail(c, AIF_ERANGE, "one call has too many queries");
     CacheList l{h, nullptr, n, bytes};
     if (far) {
         const size_t off = (size_t)slot * c->slot_bytes;

@@ -74,14 +74,16 @@ hipError_t launch_cache_fill(const CacheShape &c, const CacheList &fills, int lo
 hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStream_t s);
 
 // Attention.  A row is a query and one of the `group` heads that share a kv head; a unit is a tile of rows and one of the splits of
-// its keys.  asks: n CacheAsk, then int32 first[n + 1], running numbers of units, then int32 joins[n + 1], running numbers of the
-// rows of the asks with splits > 1.  part: room for the results of their units (CachePart).
-struct CachePlan {
+// its keys.  An entry of few rows goes to one kernel, one of many to another.  asks: n CacheAsk, then for each of the two kernels that
+// has any (few first) int32 first[n + 1], running numbers of units, and int32 joins[n + 1], running numbers of the rows whose keys are split.
+struct CachePart {
     int32_t units, joins;       // of all asks
     int32_t rows_of_tile;
-    float *part;
+    float *part;                // partial results of split keys, a unit and kv head each: [rows][dp] sums, [rows] maxima, [rows] sums of weights
 };
-// A partial result: [rows][dp] sums, then [rows] maxima and [rows] sums of weights, fp32
+struct CachePlan {
+    CachePart few, many;
+};
 __host__ __device__ inline size_t cache_part_floats(int rows, int dp) { return (size_t)rows * (dp + 2); }
 hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const CachePlan &plan, hipStream_t s);
 

@@ -17,6 +17,8 @@ struct CacheGrid {
     int32_t n, firsts;          // asks; byte offset of int32 first[n + 1]
 };
 
+void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
+
 __device__ __forceinline__ CacheAsk ask_at(const char *dev, int r)
 {
     const size_t off = (size_t)r * sizeof(CacheAsk);

@@ -240,6 +240,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
 
         if (__ballot(odd)) {
             // a row that sees a block of values that is not finite: its 32 features are NaN
+#pragma unroll 1
             for (int key = 0; key < CACHE_TILE; ++key) {
                 const int from = key & 15;
                 uint32_t bytes[4];
@@ -350,11 +351,11 @@ template <int DT> __global__ __launch_bounds__(128) void k_cache_join(CacheFew f
 }  // namespace
 
 namespace {
-template <int DT, int NW, int NT> void few(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePlan &p, hipStream_t s)
+template <int DT, int NW, int NT> void few(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
     hipLaunchKernelGGL((k_cache_few<DT, NW, NT>), dim3(p.units, c.n_kv), dim3(256), 0, s, args, dev, g, c, p.part);
 }
-template <int NW> void few_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePlan &p, hipStream_t s)
+template <int NW> void few_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
     if (c.dtype == 0) few<0, NW, 1>(args, dev, g, c, p, s);
     else if (p.rows_of_tile == 16) few<1, NW, 1>(args, dev, g, c, p, s);
@@ -362,28 +363,41 @@ template <int NW> void few_of(const CacheFew &args, const char *dev, const Cache
 }
 }  // namespace
 
+static void launch_cache_few(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
+{
+    switch (c.dp / 32) {
+    case 1: few_of<1>(args, dev, g, c, p, s); break;
+    case 2: few_of<2>(args, dev, g, c, p, s); break;
+    case 3: few_of<3>(args, dev, g, c, p, s); break;
+    case 4: few_of<4>(args, dev, g, c, p, s); break;
+    case 5: few_of<5>(args, dev, g, c, p, s); break;
+    case 6: few_of<6>(args, dev, g, c, p, s); break;
+    case 7: few_of<7>(args, dev, g, c, p, s); break;
+    default: few_of<8>(args, dev, g, c, p, s); break;
+    }
+}
+
 hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const CachePlan &p, hipStream_t s)
 {
-    if (p.units == 0) return hipSuccess;
     CacheFew args;
     if (!asks.dev) __builtin_memcpy(args.w, asks.host, asks.bytes);
     CacheGrid g{asks.n, (int32_t)(asks.n * sizeof(CacheAsk))};
-    switch (c.dp / 32) {
-    case 1: few_of<1>(args, asks.dev, g, c, p, s); break;
-    case 2: few_of<2>(args, asks.dev, g, c, p, s); break;
-    case 3: few_of<3>(args, asks.dev, g, c, p, s); break;
-    case 4: few_of<4>(args, asks.dev, g, c, p, s); break;
-    case 5: few_of<5>(args, asks.dev, g, c, p, s); break;
-    case 6: few_of<6>(args, asks.dev, g, c, p, s); break;
-    case 7: few_of<7>(args, asks.dev, g, c, p, s); break;
-    default: few_of<8>(args, asks.dev, g, c, p, s); break;
+    for (int kind = 0; kind < 2; ++kind) {
+        const CachePart &of = kind ? p.many : p.few;
+        if (of.units == 0) continue;
+        if (kind) launch_cache_many(args, asks.dev, g, c, of, s);
+        else launch_cache_few(args, asks.dev, g, c, of, s);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+        g.firsts += 4 * (asks.n + 1);
+        if (of.joins) {
+            if (c.dtype == 0) hipLaunchKernelGGL(k_cache_join<0>, dim3(of.joins, c.n_kv), dim3(128), 0, s, args, asks.dev, g, c, of.part, of.rows_of_tile);
+            else hipLaunchKernelGGL(k_cache_join<1>, dim3(of.joins, c.n_kv), dim3(128), 0, s, args, asks.dev, g, c, of.part, of.rows_of_tile);
+            if (hipError_t j = hipGetLastError(); j != hipSuccess) return j;
+        }
+        g.firsts += 4 * (asks.n + 1);
     }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || p.joins == 0) return e;
-    g.firsts += 4 * (asks.n + 1);
-    if (c.dtype == 0) hipLaunchKernelGGL(k_cache_join<0>, dim3(p.joins, c.n_kv), dim3(128), 0, s, args, asks.dev, g, c, p.part, p.rows_of_tile);
-    else hipLaunchKernelGGL(k_cache_join<1>, dim3(p.joins, c.n_kv), dim3(128), 0, s, args, asks.dev, g, c, p.part, p.rows_of_tile);
-    return hipGetLastError();
+    return hipSuccess;
 }
 
 }  // namespace aif

@@ -1,0 +1,314 @@
+// The user cache's attention for many rows (candidates): a block takes 32 CT rows a wave, 4 waves, and 64 keys a stage.
+//
+// With hundreds of rows to a key the codes are the smaller part: a stage's keys and values are brought to bf16 once for the block, 32 features
+// and their scale a thread, and lie in LDS as rows; the next stage's codes travel meanwhile, and one barrier a stage parts the two
+// buffers.  Products are 32x32x16: S^T = K Q^T with a wave's queries in registers throughout, so that a lane holds 16 keys
+// of one row, and these, as weights, are the operand of O^T = V^T P^T as they stand; V comes turned (ds_read_b64_tr_b16).  What bounds it is
+// the vector ALU: per score one fused multiply-add, half a maximum, one exponential (2.3 times a plain instruction), half a conversion and one
+// addition.
+// Rows of K are 16 bytes longer than their features, rows of V 64 (modulo 128): the lanes of a read meet different banks.
+#include "k_cache_attend.h"
+
+namespace aif {
+
+namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+constexpr float LAZY = 8.f;
+
+constexpr int k_stride(int dp) { return 2 * dp + 16; }
+constexpr int v_stride(int dp) { return (2 * dp + 63) / 128 * 128 + 64; }
+constexpr int stage_bytes(int dp) { return 2 * CACHE_TILE * (k_stride(dp) + v_stride(dp)); }
+
+template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <= 2 ? 2 : 1) void k_cache_many(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
+{
+    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 128 * CT, KST = k_stride(DP), VST = v_stride(DP);
+    constexpr int ITEMS = (128 * NW + 255) / 256;       // pieces of 32 features a thread brings to LDS per stage
+    __shared__ __align__(16) char lds[2][stage_bytes(DP)];
+    __shared__ uint8_t odd_at[2][2 * CACHE_TILE * NW];  // blocks of values that are not finite
+    __shared__ int odd_now[3];
+    (void)few;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5, kvh = blockIdx.y;
+    const int r = ask_of(dev, g, blockIdx.x, lane);
+    const CacheAsk a = ask_at(dev, r);
+    const int unit = (int)blockIdx.x - first_at(dev, g, r), row_tile = unit / a.splits, split = unit % a.splits;
+    const int n_rows = a.n_q * c.group, row0 = row_tile * ROWS;
+
+    // every wave looks over all the block's rows, for the walk; its own are [row0 + 32 CT wave, + 32 CT)
+    int lo_last = INT32_MAX, hi_last = -1, lo_from = INT32_MAX, hi_from = -1;
+    if (a.pos)
+        for (int i = lane; i < ROWS; i += 64)
+            if (row0 + i < n_rows) {
+                const Sight s = sight_of(a, (row0 + i) / c.group, true);
+                lo_last = min(lo_last, s.last);
+                hi_last = max(hi_last, s.last);
+                hi_from = max(hi_from, s.from);
+                if (s.last >= 0) lo_from = min(lo_from, s.from);
+            }
+    if (a.pos) {
+#pragma unroll
+        for (int x = 1; x < 64; x *= 2) {
+            lo_last = min(lo_last, __shfl_xor(lo_last, x));
+            hi_last = max(hi_last, __shfl_xor(hi_last, x));
+            lo_from = min(lo_from, __shfl_xor(lo_from, x));
+            hi_from = max(hi_from, __shfl_xor(hi_from, x));
+        }
+    } else {
+        const Sight s = sight_of(a, 0, true);
+        lo_last = hi_last = s.last;
+        lo_from = hi_from = s.from;
+    }
+    lo_last = __builtin_amdgcn_readfirstlane(lo_last);
+    hi_last = __builtin_amdgcn_readfirstlane(hi_last);
+    lo_from = __builtin_amdgcn_readfirstlane(lo_from);
+    hi_from = __builtin_amdgcn_readfirstlane(hi_from);
+    const Walk walk = walk_of(a, lo_last, hi_last, lo_from, hi_from);
+    const int64_t n_tiles = walk.count();
+    const int t_begin = (int)(n_tiles * split / a.splits), t_end = (int)(n_tiles * (split + 1) / a.splits);
+
+    const char *pool = c.pool + (size_t)kvh * cache_head_bytes(c);
+    const int tiles_per_page = c.page_len / CACHE_TILE;
+    auto address = [&](int t) -> const char * {         // null: behind the end, or in a page that was dropped
+        if (t >= t_end) return nullptr;
+        const int tile = walk.tile(t), page = c.table[a.entry + tile / tiles_per_page];
+        return page < 0 ? nullptr : pool + (size_t)page * c.page_bytes + (size_t)(tile % tiles_per_page) * cache_tile_bytes(DP);
+    };
+
+    // A thread's pieces of a stage of two tiles: piece id of (tile, keys or values, 32 rows, NW blocks), 16 bytes of codes and a byte.
+    uint4 raw[ITEMS];
+    uint32_t byte[ITEMS];
+    auto fetch = [&](const char *t0, const char *t1) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int id = threadIdx.x + 256 * i, b = id % (32 * NW), kv = id / (32 * NW) % 2;
+            const char *tile = id < 64 * NW ? t0 : id < 128 * NW ? t1 : nullptr;
+            raw[i] = make_uint4(0, 0, 0, 0), byte[i] = 127;
+            if (tile) {
+                raw[i] = *(const uint4 *)(tile + kv * 16 * DP + b * 16);
+                byte[i] = *(const uint8_t *)(tile + (32 + kv) * DP + b);
+            }
+        }
+    };
+    auto place = [&](int buf, int flag, int j0, int j1) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int id = threadIdx.x + 256 * i, b = id % (32 * NW), kv = id / (32 * NW) % 2, tile = id / (64 * NW);
+            if (id >= 128 * NW) break;
+            const int row = b / NW, blk = b % NW;
+            const float sc = scale_of(byte[i]);
+            const bool fine = kv == 0 || sc < 0x1p126f;         // a block of values that is not finite becomes zeros, and is noted
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+            char *to = lds[buf] + (kv ? 2 * CACHE_TILE * KST + (tile * CACHE_TILE + row) * VST : (tile * CACHE_TILE + row) * KST) + blk * 64;
+#pragma unroll
+            for (int x = 0; x < 4; ++x) ((bf16x8 *)to)[x] = decode8(fine ? w[x] : 0u, fine ? sc : 1.f);
+            if (kv) {
+                const bool seen = !fine && (tile ? j1 : j0) + row <= hi_last;
+                odd_at[buf][(tile * CACHE_TILE + row) * NW + blk] = seen;
+                odd |= seen;
+            }
+        }
+        if (odd) odd_now[flag] = 1;
+    };
+
+    // this wave's rows
+    const int w_row0 = row0 + 32 * CT * wave;
+    const bool busy = w_row0 < n_rows;
+    Sight see[CT];
+    bf16x8 q[CT][NP][KS];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+        const int row = w_row0 + 32 * t + col;
+        const bool is_row = row < n_rows;
+        const RowOf o = row_of(c, kvh, is_row ? row : 0);
+        see[t] = sight_of(a, o.i, is_row);
+        const char *qr = a.q + (size_t)o.i * a.q_stride + (size_t)o.head * c.d_head * (DT == 0 ? 4 : 2);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            bf16x8 p[NP];
+            query8<DT, NP>(qr, 16 * k + 8 * half, c.d_head, is_row, p);
+#pragma unroll
+            for (int i = 0; i < NP; ++i) q[t][i][k] = p[i];
+        }
+    }
+    f32x16 acc[CT][NW];
+    float m[CT], l[CT];
+#pragma unroll
+    for (int t = 0; t < CT; ++t) {
+        m[t] = -INFINITY, l[t] = 0.f;
+#pragma unroll
+        for (int f = 0; f < NW; ++f)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[t][f][e] = 0.f;
+    }
+    const float k2 = c.scale * LOG2E;
+    typedef s16x4 __attribute__((address_space(3))) *lds4_t;
+
+    if (threadIdx.x < 3) odd_now[threadIdx.x] = 0;
+    const char *t0 = address(t_begin), *t1 = address(t_begin + 1);
+    fetch(t0, t1);
+    __syncthreads();                                    // (odd_now)
+    place(0, 0, walk.tile(t_begin) * CACHE_TILE, walk.tile(t_begin + 1) * CACHE_TILE);
+    __syncthreads();
+    int stage = 0, flag = 0;
+    for (int t = t_begin; t < t_end; t += 2) {
+        const char *n0 = address(t + 2), *n1 = address(t + 3);
+        fetch(n0, n1);
+        const char *kb = lds[stage], *vb = kb + 2 * CACHE_TILE * KST;
+        const int odd = odd_now[flag];
+        if (busy) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                if (!(h ? t1 : t0)) continue;
+                const int tile = walk.tile(t + h), j0 = tile * CACHE_TILE + 4 * half;
+                f32x16 s[CT];
+#pragma unroll
+                for (int i = 0; i < CT; ++i)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    const bf16x8 kf = *(const bf16x8 *)(kb + (h * CACHE_TILE + col) * KST + 32 * k + 16 * half);
+#pragma unroll
+                    for (int i = 0; i < CT; ++i)
+#pragma unroll
+                        for (int p = NP - 1; p >= 0; --p) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i][p][k], s[i], 0, 0, 0);
+                }
+                const bool whole = walk.whole(tile);
+                bf16x8 weights[CT][2][NP];
+#pragma unroll
+                for (int i = 0; i < CT; ++i) {
+                    if (!whole) {
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s[i][e] = see[i].sees(j0 + 8 * (e / 4) + e % 4) ? s[i][e] : -INFINITY;
+                    }
+                    float top = -INFINITY;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
+                    top *= k2;
+                    if (__ballot(top > m[i] + LAZY)) {
+                        top = fmaxf(top, __shfl_xor(top, 32));
+                        const float m2 = fmaxf(m[i], top), back = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - m2);
+                        m[i] = m2;
+                        l[i] *= back;
+#pragma unroll
+                        for (int f = 0; f < NW; ++f) acc[i][f] *= back;
+                    }
+                    const float ref = m[i] == -INFINITY ? 0.f : m[i];
+                    float x[16];
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], k2, -ref));
+                        l[i] += x[e];
+                    }
+                    pieces8<NP>(x, weights[i][0]);
+                    pieces8<NP>(x + 8, weights[i][1]);
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int f = 0; f < NW; ++f) {
+                        // four keys of 16 features a group of 16 lanes: keys 16 k + 4 half (+ 8), features 32 f + 16 (lane / 16 % 2)
+                        const char *from = vb + (h * CACHE_TILE + 16 * k + 4 * half + (lane & 15) / 4) * VST + 64 * f + 32 * (lane >> 4 & 1) + (lane & 3) * 8;
+                        union {
+                            s16x4 h[2];
+                            bf16x8 all;
+                        } v;
+                        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)from);
+                        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(from + 8 * VST));
+#pragma unroll
+                        for (int i = 0; i < CT; ++i)
+#pragma unroll
+                            for (int p = NP - 1; p >= 0; --p) acc[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.all, weights[i][k][p], acc[i][f], 0, 0, 0);
+                    }
+                if (odd) {
+                    // a row that sees a block of values that is not finite: its features are NaN
+#pragma unroll 1
+                    for (int key = 0; key < CACHE_TILE; ++key)
+#pragma unroll
+                        for (int f = 0; f < NW; ++f) {
+                            if (!odd_at[stage][(h * CACHE_TILE + key) * NW + f]) continue;
+#pragma unroll
+                            for (int i = 0; i < CT; ++i)
+                                if (see[i].sees(tile * CACHE_TILE + key)) acc[i][f] += __builtin_nanf("");
+                        }
+                }
+            }
+        }
+        const int next = flag == 2 ? 0 : flag + 1;
+        place(stage ^ 1, next, walk.tile(t + 2) * CACHE_TILE, walk.tile(t + 3) * CACHE_TILE);
+        if (threadIdx.x == 0) odd_now[next == 2 ? 0 : next + 1] = 0;
+        t0 = n0, t1 = n1;
+        stage ^= 1, flag = next;
+        __syncthreads();
+    }
+    if (!busy) return;
+
+    float *pt = part + ((size_t)a.part + (size_t)kvh * ((n_rows + ROWS - 1) / ROWS) * a.splits + unit) * cache_part_floats(ROWS, DP);    // (splits > 1)
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+        l[i] += __shfl_xor(l[i], 32);
+        const int in_tile = 32 * CT * wave + 32 * i + col, row = row0 + in_tile;
+        if (a.splits > 1) {
+#pragma unroll
+            for (int f = 0; f < NW; ++f)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(float4 *)(pt + (size_t)in_tile * DP + 32 * f + 8 * e + 4 * half) = make_float4(acc[i][f][4 * e], acc[i][f][4 * e + 1], acc[i][f][4 * e + 2], acc[i][f][4 * e + 3]);
+            if (half == 0) pt[ROWS * DP + in_tile] = m[i], pt[ROWS * DP + ROWS + in_tile] = l[i];
+            continue;
+        }
+        if (row >= n_rows) continue;
+        const RowOf o = row_of(c, kvh, row);
+        const float over = l[i] == 0.f ? 0.f : 1.f / l[i];
+        char *out = a.out + (size_t)o.i * a.out_stride + (size_t)o.head * c.d_head * (DT == 0 ? 4 : 2);
+#pragma unroll
+        for (int f = 0; f < NW; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = 32 * f + 8 * e + 4 * half;
+                if (at >= c.d_head) continue;
+                float x[4];
+#pragma unroll
+                for (int y = 0; y < 4; ++y) x[y] = l[i] == 0.f ? 0.f : acc[i][f][4 * e + y] * over;
+                if (DT == 0) *(float4 *)(out + 4 * at) = make_float4(x[0], x[1], x[2], x[3]);
+                else *(uint2 *)(out + 2 * at) = make_uint2(f2bf(x[0]) | (uint32_t)f2bf(x[1]) << 16, f2bf(x[2]) | (uint32_t)f2bf(x[3]) << 16);
+            }
+        if (a.lse && half == 0) a.lse[(size_t)o.i * c.n_heads + o.head] = l[i] == 0.f ? -INFINITY : (m[i] + __builtin_amdgcn_logf(l[i])) * LN2;
+    }
+}
+
+template <int DT, int NW, int CT> void many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
+{
+    const dim3 grid(p.units, c.n_kv), block(256);
+    if constexpr (NW == 1)
+        if (c.d_head <= 16) {
+            hipLaunchKernelGGL((k_cache_many<DT, NW, CT, 1>), grid, block, 0, s, args, dev, g, c, p.part);
+            return;
+        }
+    hipLaunchKernelGGL((k_cache_many<DT, NW, CT, 2 * NW>), grid, block, 0, s, args, dev, g, c, p.part);
+}
+template <int NW> void many_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
+{
+    if (c.dtype == 0) many<0, NW, 1>(args, dev, g, c, p, s);
+    else if (NW <= 4 && p.rows_of_tile == 256) many<1, NW, NW <= 4 ? 2 : 1>(args, dev, g, c, p, s);
+    else many<1, NW, 1>(args, dev, g, c, p, s);
+}
+
+}  // namespace
+
+void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
+{
+    switch (c.dp / 32) {
+    case 1: many_of<1>(args, dev, g, c, p, s); break;
+    case 2: many_of<2>(args, dev, g, c, p, s); break;
+    case 3: many_of<3>(args, dev, g, c, p, s); break;
+    case 4: many_of<4>(args, dev, g, c, p, s); break;
+    case 5: many_of<5>(args, dev, g, c, p, s); break;
+    case 6: many_of<6>(args, dev, g, c, p, s); break;
+    case 7: many_of<7>(args, dev, g, c, p, s); break;
+    default: many_of<8>(args, dev, g, c, p, s); break;
+    }
+}
+
+}  // namespace aif
