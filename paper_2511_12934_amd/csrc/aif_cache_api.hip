@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cstdarg>
 #include <cstdio>
+#include <cstdlib>
 #include <exception>
 #include <new>
 #include <vector>
@@ -212,6 +213,8 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     s.d_head = f->d_head;
     s.dp = (f->d_head + CACHE_BLOCK - 1) / CACHE_BLOCK * CACHE_BLOCK;
     s.page_len = f->page_len;
+    const uint32_t tpp = f->page_len / CACHE_TILE;
+    s.tpp_magic = tpp == 1 ? 0u : (uint32_t)(((1ull << 32) + tpp - 1) / tpp);
     s.dtype = f->dtype == AIF_F32 ? 0 : 1;
     s.scale = f->scale != 0.f ? f->scale : 1.0f / __builtin_sqrtf((float)f->d_head);
     s.pages_per_seq = (int)(((int64_t)f->max_len + f->page_len - 1) / f->page_len);
@@ -382,7 +385,7 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         for (int r = 0; r < n; ++r)
             if (mine(asks[r])) most = std::max(most, rows_of(asks[r])), wide += (rows_of(asks[r]) + 255) / 256 * sh.n_kv;
         if (most == 0) continue;
-        const int rows = p.rows_of_tile = kind ? (sh.dtype == 1 && sh.dp <= 128 && wide >= 2 * c->n_cu ? 256 : 128) : (sh.dtype == 0 || most <= 16 ? 16 : 32);
+        const int rows = p.rows_of_tile = kind ? (sh.dtype == 1 && sh.dp <= 128 && wide >= 2 * c->n_cu && !getenv("T128") ? 256 : 128) : (sh.dtype == 0 || most <= 16 ? 16 : 32);
         const int64_t room = (int64_t)c->n_cu * PART_ROWS / rows;
         auto tiles_of = [&](const CacheAsk &a) { return (rows_of(a) + rows - 1) / rows; };
         int64_t work = 0, units = 0, joined = 0, parts = 0;

@@ -19,6 +19,7 @@ struct CacheShape {
     int32_t *table;             // [max_seqs, pages_per_seq]: pages of each sequence, -1 = dropped
     size_t page_bytes;
     int32_t n_heads, n_kv, group, d_head, dp, page_len, pages_per_seq, dtype;
+    uint32_t tpp_magic;         // ceil(2^32 / tiles of a page): the high word of its product with a tile (< 2^27) is the tile's page; 0: one tile a page
     float scale;
 };
 __host__ __device__ inline size_t cache_tile_bytes(int dp) { return (size_t)34 * dp; }

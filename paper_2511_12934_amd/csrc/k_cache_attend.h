@@ -88,6 +88,31 @@ __device__ __forceinline__ Walk walk_of(const CacheAsk &a, int lo_last, int hi_l
     return w;
 }
 
+// Where the tiles of a walk lie: a wave keeps 64 of them, a lane each -- tile from + step * lane of the walk --, so that the page table
+// is asked once for 64 tiles and a tile's address is two v_readlane.
+template <int DP> struct TileList {
+    uint32_t lo;
+    int32_t hi;                 // offset into the pool; below 0: none, or its page was dropped
+    int from;
+    __device__ __forceinline__ void fill(const CacheShape &c, const CacheAsk &a, const Walk &w, int first, int step, int end, int lane)
+    {
+        from = first;
+        const int t = first + step * lane;
+        int64_t off = -1;
+        if (t < end) {
+            const uint32_t tile = w.tile(t), i = c.tpp_magic ? __umulhi(tile, c.tpp_magic) : tile;
+            const int page = as_global(c.table)[a.entry + (int)i];
+            if (page >= 0) off = (int64_t)page * c.page_bytes + (tile - i * (uint32_t)(c.page_len / CACHE_TILE)) * (uint32_t)cache_tile_bytes(DP);
+        }
+        lo = (uint32_t)off;
+        hi = (int32_t)(off >> 32);
+    }
+    __device__ __forceinline__ int64_t offset(int i) const       // i in 0..63
+    {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane(hi, i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)lo, i));
+    }
+};
+
 // Eight codes as bf16, times 2^(byte - 127) (a byte of 255 gives NaN).
 __device__ __forceinline__ bf16x8 decode8(uint32_t codes, float scale)
 {

@@ -132,13 +132,6 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     const int t_end = (int)(n_tiles * (split + 1) / a.splits);
 
     const char *pool = c.pool + (size_t)kvh * cache_head_bytes(c);
-    const int tiles_per_page = c.page_len / CACHE_TILE;
-    // tile t of the walk, or null: it lies in a page that was dropped
-    auto address = [&](int t) -> const char * {
-        const int tile = walk.tile(t), page = c.table[a.entry + tile / tiles_per_page];
-        return page < 0 ? nullptr : pool + (size_t)page * c.page_bytes + (size_t)(tile % tiles_per_page) * cache_tile_bytes(DP);
-    };
-
     f32x4 acc[NT][FT];
     float m[NT], l[NT];
 #pragma unroll
@@ -153,14 +146,21 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     const char *turned = mine + (4 * grp + col / 4) * STRIDE + col % 4 * 8;      // this lane's piece of four keys and 16 features
 
     int t = (int)(n_tiles * split / a.splits) + wave;
+    TileList<DP> list;
+    list.fill(c, a, walk, t, 4, t_end, lane);
+    // tile list.from + 4 i; one that is dropped or behind the end reads page 0
+    auto ask = [&](int i, RawTile<NW> &to) {
+        const int64_t off = list.offset(i);
+        load_tile<NW>(pool + (off < 0 ? 0 : off), lane, to);
+        return off >= 0;
+    };
     RawTile<NW> raw;
-    const char *at = t < t_end ? address(t) : nullptr;
-    if (at) load_tile<NW>(at, lane, raw);
-    for (; t < t_end; t += 4) {
+    bool next = ask(0, raw);
+    for (int i = 1; t < t_end; t += 4, ++i) {
         const RawTile<NW> now = raw;
-        const bool here = at != nullptr;
-        at = t + 4 < t_end ? address(t + 4) : nullptr;
-        if (at) load_tile<NW>(at, lane, raw);
+        const bool here = next;
+        if (i == 64) list.fill(c, a, walk, t + 4, 4, t_end, lane), i = 0;
+        next = ask(i, raw);
         if (!here) continue;
         const int tile = walk.tile(t), j0 = tile * CACHE_TILE + 4 * grp;
 

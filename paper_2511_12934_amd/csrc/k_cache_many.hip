@@ -20,13 +20,12 @@ constexpr int k_stride(int dp) { return 2 * dp + 16; }
 constexpr int v_stride(int dp) { return (2 * dp + 63) / 128 * 128 + 64; }
 constexpr int stage_bytes(int dp) { return 2 * CACHE_TILE * (k_stride(dp) + v_stride(dp)); }
 
-template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <= 2 ? 2 : 1) void k_cache_many(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
+template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? (NW <= 2 ? 4 : 2) : NW <= 2 ? 2 : 1) void k_cache_many(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
 {
-    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 128 * CT, KST = k_stride(DP), VST = v_stride(DP);
-    constexpr int ITEMS = (128 * NW + 255) / 256;       // pieces of 32 features a thread brings to LDS per stage
+    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 32 * WAVES * CT, THREADS = 64 * WAVES, KST = k_stride(DP), VST = v_stride(DP);
+    constexpr int ITEMS = (128 * NW + THREADS - 1) / THREADS;       // pieces of 32 features a thread brings to LDS per stage
     __shared__ __align__(16) char lds[2][stage_bytes(DP)];
-    __shared__ uint8_t odd_at[2][2 * CACHE_TILE * NW];  // blocks of values that are not finite
-    __shared__ int odd_now[3];
+    __shared__ int odd_now[3];                          // whether a stage has blocks of values that are not finite
     (void)few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5, kvh = blockIdx.y;
     const int r = ask_of(dev, g, blockIdx.x, lane);
@@ -67,46 +66,51 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <
     const int t_begin = (int)(n_tiles * split / a.splits), t_end = (int)(n_tiles * (split + 1) / a.splits);
 
     const char *pool = c.pool + (size_t)kvh * cache_head_bytes(c);
-    const int tiles_per_page = c.page_len / CACHE_TILE;
-    auto address = [&](int t) -> const char * {         // null: behind the end, or in a page that was dropped
-        if (t >= t_end) return nullptr;
-        const int tile = walk.tile(t), page = c.table[a.entry + tile / tiles_per_page];
-        return page < 0 ? nullptr : pool + (size_t)page * c.page_bytes + (size_t)(tile % tiles_per_page) * cache_tile_bytes(DP);
+    TileList<DP> list;
+    list.fill(c, a, walk, t_begin, 1, t_end, lane);
+    // tile t of the walk (t - list.from in 0..63); dead: behind the end, or in a page that was dropped.  A dead tile reads
+    // page 0, which nobody sees.
+    auto locate = [&](int t, bool &dead) {
+        const int64_t off = list.offset(t - list.from);
+        dead = off < 0;
+        return pool + (dead ? 0 : off);
     };
 
     // A thread's pieces of a stage of two tiles: piece id of (tile, keys or values, 32 rows, NW blocks), 16 bytes of codes and a byte.
+    // Which tile is the same for a wave's lanes, and so is, NW even, which of keys and values.
     uint4 raw[ITEMS];
     uint32_t byte[ITEMS];
     auto fetch = [&](const char *t0, const char *t1) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int id = threadIdx.x + 256 * i, b = id % (32 * NW), kv = id / (32 * NW) % 2;
-            const char *tile = id < 64 * NW ? t0 : id < 128 * NW ? t1 : nullptr;
-            raw[i] = make_uint4(0, 0, 0, 0), byte[i] = 127;
-            if (tile) {
-                raw[i] = *(const uint4 *)(tile + kv * 16 * DP + b * 16);
-                byte[i] = *(const uint8_t *)(tile + (32 + kv) * DP + b);
-            }
+            const int id64 = (wave + WAVES * i) * 64, id = id64 + lane, b = id % (32 * NW), kv = id / (32 * NW) % 2;
+            if (id64 >= 128 * NW) break;
+            const char *tile = as_global(id64 < 64 * NW ? t0 : t1);
+            raw[i] = *(const uint4 *)(tile + (uint32_t)(kv * 16 * DP + b * 16));
+            byte[i] = *(const uint8_t *)(tile + (uint32_t)((32 + kv) * DP + b));
         }
     };
-    auto place = [&](int buf, int flag, int j0, int j1) {
+    auto place = [&](int buf, int flag, int j0, int j1) {       // j0, j1: the tiles' first keys, beyond every row's where one is dead
         bool odd = false;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int id = threadIdx.x + 256 * i, b = id % (32 * NW), kv = id / (32 * NW) % 2, tile = id / (64 * NW);
-            if (id >= 128 * NW) break;
+            const int id64 = (wave + WAVES * i) * 64, id = id64 + lane, b = id % (32 * NW), tile = id64 / (64 * NW);
+            if (id64 >= 128 * NW) break;
+            const bool vals = NW % 2 == 0 ? id64 / (32 * NW) % 2 : id / (32 * NW) % 2;
             const int row = b / NW, blk = b % NW;
-            const float sc = scale_of(byte[i]);
-            const bool fine = kv == 0 || sc < 0x1p126f;         // a block of values that is not finite becomes zeros, and is noted
-            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-            char *to = lds[buf] + (kv ? 2 * CACHE_TILE * KST + (tile * CACHE_TILE + row) * VST : (tile * CACHE_TILE + row) * KST) + blk * 64;
-#pragma unroll
-            for (int x = 0; x < 4; ++x) ((bf16x8 *)to)[x] = decode8(fine ? w[x] : 0u, fine ? sc : 1.f);
-            if (kv) {
-                const bool seen = !fine && (tile ? j1 : j0) + row <= hi_last;
-                odd_at[buf][(tile * CACHE_TILE + row) * NW + blk] = seen;
-                odd |= seen;
+            asm volatile("" : "+v"(byte[i]));              // (what is made of a byte is made here, not where it is asked for: that would wait for it)
+            float sc = scale_of(byte[i]);
+            if (vals) {                                     // a block of values that is not finite becomes zeros, and is noted
+                const bool fine = sc < 0x1p126f;
+                odd |= !fine && (tile ? j1 : j0) + row <= hi_last;
+                sc = fine ? sc : 1.f;
+                raw[i].x = fine ? raw[i].x : 0u, raw[i].y = fine ? raw[i].y : 0u, raw[i].z = fine ? raw[i].z : 0u, raw[i].w = fine ? raw[i].w : 0u;
             }
+            bf16x8 *to = (bf16x8 *)(lds[buf] + (vals ? 2 * CACHE_TILE * KST + (tile * CACHE_TILE + row) * VST : (tile * CACHE_TILE + row) * KST) + blk * 64);
+            to[0] = decode8(raw[i].x, sc);
+            to[1] = decode8(raw[i].y, sc);
+            to[2] = decode8(raw[i].z, sc);
+            to[3] = decode8(raw[i].w, sc);
         }
         if (odd) odd_now[flag] = 1;
     };
@@ -145,21 +149,26 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <
     typedef s16x4 __attribute__((address_space(3))) *lds4_t;
 
     if (threadIdx.x < 3) odd_now[threadIdx.x] = 0;
-    const char *t0 = address(t_begin), *t1 = address(t_begin + 1);
+    if (t_begin < t_end) {
+    bool dead0, dead1;
+    const char *t0 = locate(t_begin, dead0), *t1 = locate(t_begin + 1, dead1);
+    auto first_key = [&](int t, bool dead) { return dead ? INT32_MAX - CACHE_TILE : walk.tile(t) * CACHE_TILE; };
     fetch(t0, t1);
     __syncthreads();                                    // (odd_now)
-    place(0, 0, walk.tile(t_begin) * CACHE_TILE, walk.tile(t_begin + 1) * CACHE_TILE);
+    place(0, 0, first_key(t_begin, dead0), first_key(t_begin + 1, dead1));
     __syncthreads();
     int stage = 0, flag = 0;
     for (int t = t_begin; t < t_end; t += 2) {
-        const char *n0 = address(t + 2), *n1 = address(t + 3);
+        if (t + 2 - list.from >= 64) list.fill(c, a, walk, t + 2, 1, t_end, lane);
+        bool next_dead0, next_dead1;
+        const char *n0 = locate(t + 2, next_dead0), *n1 = locate(t + 3, next_dead1);
         fetch(n0, n1);
         const char *kb = lds[stage], *vb = kb + 2 * CACHE_TILE * KST;
         const int odd = odd_now[flag];
         if (busy) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                if (!(h ? t1 : t0)) continue;
+                if (h ? dead1 : dead0) continue;
                 const int tile = walk.tile(t + h), j0 = tile * CACHE_TILE + 4 * half;
                 f32x16 s[CT];
 #pragma unroll
@@ -179,8 +188,15 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <
 #pragma unroll
                 for (int i = 0; i < CT; ++i) {
                     if (!whole) {
+                        if (tile * CACHE_TILE >= walk.sinks) {          // one run of keys
+                            const uint32_t at = j0 - see[i].from, span = see[i].last - see[i].from;
+                            const bool any = see[i].last >= see[i].from;
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) s[i][e] = see[i].sees(j0 + 8 * (e / 4) + e % 4) ? s[i][e] : -INFINITY;
+                            for (int e = 0; e < 16; ++e) s[i][e] = any && at + 8 * (e / 4) + e % 4 <= span ? s[i][e] : -INFINITY;
+                        } else {
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) s[i][e] = see[i].sees(j0 + 8 * (e / 4) + e % 4) ? s[i][e] : -INFINITY;
+                        }
                     }
                     float top = -INFINITY;
 #pragma unroll
@@ -227,7 +243,7 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <
                     for (int key = 0; key < CACHE_TILE; ++key)
 #pragma unroll
                         for (int f = 0; f < NW; ++f) {
-                            if (!odd_at[stage][(h * CACHE_TILE + key) * NW + f]) continue;
+                            if (scale_of(*(const uint8_t *)((h ? t1 : t0) + 33 * DP + key * NW + f)) < 0x1p126f) continue;
 #pragma unroll
                             for (int i = 0; i < CT; ++i)
                                 if (see[i].sees(tile * CACHE_TILE + key)) acc[i][f] += __builtin_nanf("");
@@ -236,11 +252,13 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <
             }
         }
         const int next = flag == 2 ? 0 : flag + 1;
-        place(stage ^ 1, next, walk.tile(t + 2) * CACHE_TILE, walk.tile(t + 3) * CACHE_TILE);
+        place(stage ^ 1, next, first_key(t + 2, next_dead0), first_key(t + 3, next_dead1));
         if (threadIdx.x == 0) odd_now[next == 2 ? 0 : next + 1] = 0;
         t0 = n0, t1 = n1;
+        dead0 = next_dead0, dead1 = next_dead1;
         stage ^= 1, flag = next;
         __syncthreads();
+    }
     }
     if (!busy) return;
 
@@ -278,21 +296,21 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, NW <
     }
 }
 
-template <int DT, int NW, int CT> void many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
+template <int DT, int NW, int CT, int WAVES> void many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
-    const dim3 grid(p.units, c.n_kv), block(256);
+    const dim3 grid(p.units, c.n_kv), block(64 * WAVES);
     if constexpr (NW == 1)
         if (c.d_head <= 16) {
-            hipLaunchKernelGGL((k_cache_many<DT, NW, CT, 1>), grid, block, 0, s, args, dev, g, c, p.part);
+            hipLaunchKernelGGL((k_cache_many<DT, NW, CT, WAVES, 1>), grid, block, 0, s, args, dev, g, c, p.part);
             return;
         }
-    hipLaunchKernelGGL((k_cache_many<DT, NW, CT, 2 * NW>), grid, block, 0, s, args, dev, g, c, p.part);
+    hipLaunchKernelGGL((k_cache_many<DT, NW, CT, WAVES, 2 * NW>), grid, block, 0, s, args, dev, g, c, p.part);
 }
 template <int NW> void many_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
-    if (c.dtype == 0) many<0, NW, 1>(args, dev, g, c, p, s);
-    else if (NW <= 4 && p.rows_of_tile == 256) many<1, NW, NW <= 4 ? 2 : 1>(args, dev, g, c, p, s);
-    else many<1, NW, 1>(args, dev, g, c, p, s);
+    if (c.dtype == 0) many<0, NW, 1, 4>(args, dev, g, c, p, s);
+    else if (NW <= 4 && p.rows_of_tile == 256) many<1, NW, NW <= 2 ? 1 : NW <= 4 ? 2 : 1, NW <= 2 ? 8 : 4>(args, dev, g, c, p, s);
+    else many<1, NW, 1, 4>(args, dev, g, c, p, s);
 }
 
 }  // namespace
