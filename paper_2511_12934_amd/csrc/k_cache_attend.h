@@ -6,10 +6,13 @@
 namespace aif {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
+constexpr float LAZY = 8.f;             // how far, in powers of two, a score may pass the reference of its row's weights
 constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 
 // The blocks of a launch: running numbers of units behind the asks.  A unit is (row tile, split), tiles first.
@@ -17,6 +20,7 @@ struct CacheGrid {
     int32_t n, firsts;          // asks; byte offset of int32 first[n + 1]
 };
 
+void launch_cache_own(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
 void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
 
 __device__ __forceinline__ CacheAsk ask_at(const char *dev, int r)
@@ -47,6 +51,18 @@ __device__ __forceinline__ int ask_of(const char *dev, const CacheGrid &g, int u
 struct Sight {
     int last, from, sinks;
     __device__ __forceinline__ bool sees(int j) const { return j <= last && (j >= from || j < sinks); }
+    // scores of the keys j0 + 8 (e / 4) + e % 4 of a tile: minus infinity where not seen
+    __device__ __forceinline__ void hide(f32x16 &s, int j0, int tile, int all_sinks) const
+    {
+        if (tile * CACHE_TILE >= all_sinks) {               // one run of keys, [from, last]
+            const uint32_t at = (uint32_t)j0 - (uint32_t)from, span = last >= from ? last - from + 1 : 0;      // last - from < window
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = at + 8 * (e / 4) + e % 4 < span ? s[e] : -INFINITY;
+        } else {
+#pragma unroll
+            for (int e = 0; e < 16; ++e) s[e] = sees(j0 + 8 * (e / 4) + e % 4) ? s[e] : -INFINITY;
+        }
+    }
 };
 __device__ __forceinline__ Sight sight_of(const CacheAsk &a, int i, bool is_row)
 {
@@ -72,21 +88,44 @@ struct Walk {
         return j + CACHE_TILE - 1 <= all_last && (j >= all_from || j + CACHE_TILE <= sinks);
     }
 };
-// min / max over the rows that see anything at all (last >= 0); lo_*: the smallest, hi_*: the largest
-__device__ __forceinline__ Walk walk_of(const CacheAsk &a, int lo_last, int hi_last, int lo_from, int hi_from)
-{
-    Walk w;
-    w.sinks = a.window ? a.sinks : 0;
-    w.all_last = lo_last;
-    w.all_from = hi_from;
-    w.end = (hi_last + CACHE_TILE) / CACHE_TILE;            // hi_last = -1: none
-    w.body = (lo_from > 0 ? lo_from : 0) / CACHE_TILE;
-    const int s = w.sinks < hi_last + 1 ? w.sinks : hi_last + 1;
-    const int head = (s + CACHE_TILE - 1) / CACHE_TILE;
-    w.body = w.body < w.end ? w.body : w.end;
-    w.head = head < w.body ? head : w.body;
-    return w;
-}
+// What the rows of a wave or block see together.
+struct Reach {
+    int lo_last = INT32_MAX, hi_last = -1, lo_from = INT32_MAX, hi_from = INT32_MIN;
+    __device__ __forceinline__ void add(const Sight &s, bool is_row)
+    {
+        if (!is_row) return;
+        lo_last = min(lo_last, s.last);
+        hi_last = max(hi_last, s.last);
+        hi_from = max(hi_from, s.from);
+        if (s.last >= 0) lo_from = min(lo_from, s.from);    // (one that sees nothing widens nothing)
+    }
+    // the tiles, of the rows that LANES neighbouring lanes have added (the same in every such group); all lanes alike
+    template <int LANES> __device__ __forceinline__ Walk walk(const CacheAsk &a)
+    {
+        if (a.pos) {                                        // else every row sees the same
+#pragma unroll
+            for (int x = 1; x < LANES; x *= 2) {
+                lo_last = min(lo_last, __shfl_xor(lo_last, x));
+                hi_last = max(hi_last, __shfl_xor(hi_last, x));
+                lo_from = min(lo_from, __shfl_xor(lo_from, x));
+                hi_from = max(hi_from, __shfl_xor(hi_from, x));
+            }
+        }
+        // (lane 0 has a row wherever a lane has one)
+        lo_last = __builtin_amdgcn_readfirstlane(lo_last);
+        hi_last = __builtin_amdgcn_readfirstlane(hi_last);
+        lo_from = __builtin_amdgcn_readfirstlane(lo_from);
+        hi_from = __builtin_amdgcn_readfirstlane(hi_from);
+        Walk w;
+        w.sinks = a.window ? a.sinks : 0;
+        w.all_last = lo_last;
+        w.all_from = hi_from;
+        w.end = (hi_last + CACHE_TILE) / CACHE_TILE;        // hi_last = -1: none
+        w.body = min((lo_from > 0 ? lo_from : 0) / CACHE_TILE, w.end);
+        w.head = min((min(w.sinks, hi_last + 1) + CACHE_TILE - 1) / CACHE_TILE, w.body);
+        return w;
+    }
+};
 
 // Where the tiles of a walk lie: a wave keeps 64 of them, a lane each -- tile from + step * lane of the walk --, so that the page table
 // is asked once for 64 tiles and a tile's address is two v_readlane.
@@ -174,5 +213,53 @@ struct RowOf {
     int i, head;
 };
 __device__ __forceinline__ RowOf row_of(const CacheShape &c, int kvh, int row) { return RowOf{row / c.group, kvh * c.group + row % c.group}; }
+
+// Rows of values in LDS, whose parts are read four keys at a time: 64 bytes (modulo 128) apart, so that these lie in different banks.
+constexpr int v_stride(int dp) { return (2 * dp + 63) / 128 * 128 + 64; }
+
+// The end of a wave's rows in_block + 32 i + col of a block's ROWS from `row0` on: quotients and logarithms, or a part for the join.  A lane holds
+// the features 32 f + 8 (e / 4) + 4 half + e % 4 of its row, and its own share of the sum l.
+template <int DT, int NW, int CT, int ROWS>
+__device__ __forceinline__ void finish_rows(const CacheAsk &a, const CacheShape &c, float *part, int kvh, int unit, int n_rows, int row0, int in_block, int col, int half,
+                                            f32x16 (&acc)[CT][NW], const float (&m)[CT], float (&l)[CT])
+{
+    constexpr int DP = 32 * NW;
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {
+        l[i] += __shfl_xor(l[i], 32);
+        const int at = in_block + 32 * i + col, row = row0 + at;
+        if (a.splits > 1) {
+            float *pt = part + ((size_t)a.part + (size_t)kvh * ((n_rows + ROWS - 1) / ROWS) * a.splits + unit) * cache_part_floats(ROWS, DP);
+#pragma unroll
+            for (int f = 0; f < NW; ++f)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(float4 *)(pt + (size_t)at * DP + 32 * f + 8 * e + 4 * half) = make_float4(acc[i][f][4 * e], acc[i][f][4 * e + 1], acc[i][f][4 * e + 2], acc[i][f][4 * e + 3]);
+            if (half == 0) pt[ROWS * DP + at] = m[i], pt[ROWS * DP + ROWS + at] = l[i];
+            continue;
+        }
+        if (row >= n_rows) continue;
+        if (l[i] == 0.f) {                      // no key, or scores of minus infinity alone
+#pragma unroll
+            for (int f = 0; f < NW; ++f)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][f][e] = 0.f;
+        }
+        const RowOf o = row_of(c, kvh, row);
+        const float over = l[i] == 0.f ? 0.f : 1.f / l[i];
+        char *out = as_global(a.out) + (size_t)o.i * a.out_stride + ((size_t)o.head * c.d_head + 4 * half) * (DT == 0 ? 4 : 2);
+#pragma unroll
+        for (int f = 0; f < NW; ++f)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int first = 32 * f + 8 * e;
+                if (first >= c.d_head || (DT == 0 && first + 4 * half >= c.d_head)) continue;
+                f32x4 x = f32x4{acc[i][f][4 * e], acc[i][f][4 * e + 1], acc[i][f][4 * e + 2], acc[i][f][4 * e + 3]} * over;
+                if constexpr (DT == 0) *(f32x4 *)(out + 4 * first) = x;
+                else *(bf16x4 *)(out + 2 * first) = __builtin_convertvector(x, bf16x4);
+            }
+        if (a.lse && half == 0) as_global(a.lse)[(size_t)o.i * c.n_heads + o.head] = l[i] == 0.f ? -INFINITY : (m[i] + __builtin_amdgcn_logf(l[i])) * LN2;
+    }
+}
 
 }  // namespace aif

@@ -19,11 +19,20 @@ namespace aif {
 
 namespace {
 
-constexpr float LAZY = 8.f;             // how far, in powers of two, a score may pass the reference
-
 // What a lane holds of a tile: of key lane % 16 (+ 16) the features [lane / 16 * dp / 4, + dp / 4), NW words of eight.
+// (blocks that a lane's NW words can lie in)
+template <int NW> constexpr int blocks_of() { return NW == 7 ? 3 : NW == 3 || NW > 4 ? 2 : 1; }
 template <int NW> struct RawTile {
-    uint32_t k[2][NW], v[2][NW], ks[2], vs[2];      // ks, vs: up to four scale bytes, from the first block of the lane's features on
+    uint32_t k[2][NW], v[2][NW], ks[2][blocks_of<NW>()], vs[2][blocks_of<NW>()];    // ks, vs: scale bytes, from the first block of the lane's features on
+    bool here;
+    // what is made of the bytes is made behind this, not where they are asked for: that would wait for them
+    __device__ __forceinline__ void pin()
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int b = 0; b < blocks_of<NW>(); ++b) asm volatile("" : "+v"(ks[h][b]), "+v"(vs[h][b]));
+    }
 };
 
 template <int NW> __device__ __forceinline__ void load_words(const char *p, uint32_t *w)
@@ -46,9 +55,6 @@ template <int NW> __device__ __forceinline__ void load_words(const char *p, uint
     }
 }
 
-// blocks that a lane's NW words can lie in
-template <int NW> constexpr int blocks_of() { return NW == 7 ? 3 : NW == 3 || NW > 4 ? 2 : 1; }
-
 template <int NW> __device__ __forceinline__ void load_tile(const char *tile, int lane, RawTile<NW> &r)
 {
     constexpr int DP = 32 * NW;
@@ -59,22 +65,27 @@ template <int NW> __device__ __forceinline__ void load_tile(const char *tile, in
         load_words<NW>(tile + row * (DP / 2) + grp * (DP / 8), r.k[h]);
         load_words<NW>(tile + 16 * DP + row * (DP / 2) + grp * (DP / 8), r.v[h]);
         const uint8_t *ks = (const uint8_t *)tile + 32 * DP + row * NW, *vs = ks + DP;
-        r.ks[h] = ks[lo], r.vs[h] = vs[lo];
 #pragma unroll
-        for (int b = 1; b < blocks_of<NW>(); ++b) {         // (the last group's last bytes may be the next row's: not used then)
+        for (int b = 0; b < blocks_of<NW>(); ++b) {         // (the last group may hold fewer blocks)
             const int at = lo + b < NW ? lo + b : NW - 1;
-            r.ks[h] |= (uint32_t)ks[at] << (8 * b);
-            r.vs[h] |= (uint32_t)vs[at] << (8 * b);
+            r.ks[h][b] = ks[at];
+            r.vs[h][b] = vs[at];
         }
     }
 }
 
 // the scale of word w of a lane's NW
-template <int NW> __device__ __forceinline__ float word_scale(uint32_t bytes, int grp, int w)
+template <int NW> __device__ __forceinline__ float word_scale(const uint32_t (&bytes)[blocks_of<NW>()], int grp, int w)
 {
-    if constexpr (blocks_of<NW>() == 1) return scale_of(bytes);
-    else if constexpr (NW == 8) return scale_of((bytes >> (w / 4 * 8)) & 255);
-    else return scale_of((bytes >> (((grp * NW + w) / 4 - grp * NW / 4) * 8)) & 255);
+    uint32_t b = bytes[0];
+    if constexpr (NW == 8) b = bytes[w / 4];
+    else if constexpr (blocks_of<NW>() > 1) {
+        const int i = (grp * NW + w) / 4 - grp * NW / 4;
+        if (i == 1) b = bytes[1];
+        if constexpr (blocks_of<NW>() > 2)
+            if (i == 2) b = bytes[2];
+    }
+    return scale_of(b);
 }
 
 template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache_few(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
@@ -94,19 +105,14 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     // the rows: who sees what, and their features
     Sight see[NT];
     bf16x8 q[NT][NP][NW];
-    int lo_last = INT32_MAX, hi_last = -1, lo_from = INT32_MAX, hi_from = -1;
+    Reach reach;
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
         const int row = row0 + 16 * t + col;
         const bool is_row = row < n_rows;
         const RowOf o = row_of(c, kvh, is_row ? row : 0);
         see[t] = sight_of(a, o.i, is_row);
-        if (is_row) {
-            lo_last = min(lo_last, see[t].last);
-            hi_last = max(hi_last, see[t].last);
-            hi_from = max(hi_from, see[t].from);
-            if (see[t].last >= 0) lo_from = min(lo_from, see[t].from);
-        }
+        reach.add(see[t], is_row);
         const char *qr = a.q + (size_t)o.i * a.q_stride + (size_t)o.head * c.d_head * (DT == 0 ? 4 : 2);
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
@@ -116,18 +122,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
             for (int i = 0; i < NP; ++i) q[t][i][w] = p[i];
         }
     }
-#pragma unroll
-    for (int x = 1; x < 16; x *= 2) {
-        lo_last = min(lo_last, __shfl_xor(lo_last, x));
-        hi_last = max(hi_last, __shfl_xor(hi_last, x));
-        lo_from = min(lo_from, __shfl_xor(lo_from, x));
-        hi_from = max(hi_from, __shfl_xor(hi_from, x));
-    }
-    lo_last = __builtin_amdgcn_readfirstlane(lo_last);
-    hi_last = __builtin_amdgcn_readfirstlane(hi_last);
-    lo_from = __builtin_amdgcn_readfirstlane(lo_from);
-    hi_from = __builtin_amdgcn_readfirstlane(hi_from);
-    const Walk walk = walk_of(a, lo_last, hi_last, lo_from, hi_from);
+    const Walk walk = reach.walk<16>(a);
     const int64_t n_tiles = walk.count();
     const int t_end = (int)(n_tiles * (split + 1) / a.splits);
 
@@ -148,20 +143,15 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     int t = (int)(n_tiles * split / a.splits) + wave;
     TileList<DP> list;
     list.fill(c, a, walk, t, 4, t_end, lane);
-    // tile list.from + 4 i; one that is dropped or behind the end reads page 0
-    auto ask = [&](int i, RawTile<NW> &to) {
-        const int64_t off = list.offset(i);
+    auto ask = [&](int t, RawTile<NW> &to) {            // a tile that is dropped or behind the end reads page 0
+        if (t - list.from == 256) list.fill(c, a, walk, t, 4, t_end, lane);
+        const int64_t off = list.offset((t - list.from) / 4);
+        to.here = off >= 0;
         load_tile<NW>(pool + (off < 0 ? 0 : off), lane, to);
-        return off >= 0;
     };
-    RawTile<NW> raw;
-    bool next = ask(0, raw);
-    for (int i = 1; t < t_end; t += 4, ++i) {
-        const RawTile<NW> now = raw;
-        const bool here = next;
-        if (i == 64) list.fill(c, a, walk, t + 4, 4, t_end, lane), i = 0;
-        next = ask(i, raw);
-        if (!here) continue;
+    auto work = [&](int t, RawTile<NW> &now) {
+        if (!now.here) return;
+        now.pin();
         const int tile = walk.tile(t), j0 = tile * CACHE_TILE + 4 * grp;
 
         // values: as bf16 rows of the wave's LDS.  A block that is not finite -- NaN, or bytes that nobody wrote -- becomes zeros:
@@ -173,7 +163,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
             for (int w = 0; w < NW; ++w) {
                 const float sc = word_scale<NW>(now.vs[h], grp, w);
                 const bool fine = sc < 0x1p126f;
-                odd |= fine || tile * CACHE_TILE + 16 * h + col > hi_last ? 0u : 1u;
+                odd |= fine || tile * CACHE_TILE + 16 * h + col > reach.hi_last ? 0u : 1u;
                 *(bf16x8 *)(mine + (16 * h + col) * STRIDE + (grp * (DP / 4) + 8 * w) * 2) = decode8(fine ? now.v[h][w] : 0u, fine ? sc : 1.f);
             }
         }
@@ -243,20 +233,26 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
 #pragma unroll 1
             for (int key = 0; key < CACHE_TILE; ++key) {
                 const int from = key & 15;
-                uint32_t bytes[4];
-                #pragma unroll
-                for (int gr = 0; gr < 4; ++gr) bytes[gr] = __shfl(key < 16 ? now.vs[0] : now.vs[1], from + 16 * gr);
 #pragma unroll
-                for (int f = 0; f < FT; ++f) {              // 16 features of block f / 2, which group f / 2 * 4 / NW holds
-                    const int gr = f / 2 * 4 / NW, lo = gr * NW / 4;
-                    const float sc = scale_of((bytes[gr] >> ((f / 2 - lo) * 8)) & 255);
-                    if (sc < 0x1p126f) continue;
+                for (int f = 0; f < FT; ++f) {              // 16 features of block f / 2, whose first word group f / 2 * 4 / NW holds
+                    const int gr = f / 2 * 4 / NW, b = f / 2 - gr * NW / 4;
+                    const uint32_t byte = __shfl(key < 16 ? now.vs[0][b] : now.vs[1][b], from + 16 * gr);
+                    if (scale_of(byte) < 0x1p126f) continue;
 #pragma unroll
                     for (int i = 0; i < NT; ++i)
                         if (see[i].sees(tile * CACHE_TILE + key)) acc[i][f] += __builtin_nanf("");
                 }
             }
         }
+    };
+    // two sets of registers by turns: what one is loaded with is not waited for while the other is worked on
+    RawTile<NW> raw0, raw1;
+    ask(t, raw0);
+    for (; t < t_end; t += 8) {
+        ask(t + 4, raw1);
+        work(t, raw0);
+        ask(t + 8, raw0);
+        if (t + 4 < t_end) work(t + 4, raw1);
     }
 
     // the four waves' parts become one: a common reference, then sums through LDS
@@ -385,7 +381,8 @@ hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const
     for (int kind = 0; kind < 2; ++kind) {
         const CachePart &of = kind ? p.many : p.few;
         if (of.units == 0) continue;
-        if (kind) launch_cache_many(args, asks.dev, g, c, of, s);
+        if (kind && c.dp <= 64) launch_cache_own(args, asks.dev, g, c, of, s);
+        else if (kind) launch_cache_many(args, asks.dev, g, c, of, s);
         else launch_cache_few(args, asks.dev, g, c, of, s);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

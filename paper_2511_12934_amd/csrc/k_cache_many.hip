@@ -13,11 +13,8 @@ namespace aif {
 
 namespace {
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-constexpr float LAZY = 8.f;
 
 constexpr int k_stride(int dp) { return 2 * dp + 16; }
-constexpr int v_stride(int dp) { return (2 * dp + 63) / 128 * 128 + 64; }
 constexpr int stage_bytes(int dp) { return 2 * CACHE_TILE * (k_stride(dp) + v_stride(dp)); }
 
 template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? (NW <= 2 ? 4 : 2) : NW <= 2 ? 2 : 1) void k_cache_many(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
@@ -34,34 +31,14 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
     const int n_rows = a.n_q * c.group, row0 = row_tile * ROWS;
 
     // every wave looks over all the block's rows, for the walk; its own are [row0 + 32 CT wave, + 32 CT)
-    int lo_last = INT32_MAX, hi_last = -1, lo_from = INT32_MAX, hi_from = -1;
-    if (a.pos)
-        for (int i = lane; i < ROWS; i += 64)
-            if (row0 + i < n_rows) {
-                const Sight s = sight_of(a, (row0 + i) / c.group, true);
-                lo_last = min(lo_last, s.last);
-                hi_last = max(hi_last, s.last);
-                hi_from = max(hi_from, s.from);
-                if (s.last >= 0) lo_from = min(lo_from, s.from);
-            }
+    Reach reach;
     if (a.pos) {
-#pragma unroll
-        for (int x = 1; x < 64; x *= 2) {
-            lo_last = min(lo_last, __shfl_xor(lo_last, x));
-            hi_last = max(hi_last, __shfl_xor(hi_last, x));
-            lo_from = min(lo_from, __shfl_xor(lo_from, x));
-            hi_from = max(hi_from, __shfl_xor(hi_from, x));
-        }
-    } else {
-        const Sight s = sight_of(a, 0, true);
-        lo_last = hi_last = s.last;
-        lo_from = hi_from = s.from;
-    }
-    lo_last = __builtin_amdgcn_readfirstlane(lo_last);
-    hi_last = __builtin_amdgcn_readfirstlane(hi_last);
-    lo_from = __builtin_amdgcn_readfirstlane(lo_from);
-    hi_from = __builtin_amdgcn_readfirstlane(hi_from);
-    const Walk walk = walk_of(a, lo_last, hi_last, lo_from, hi_from);
+        for (int i = lane; i < ROWS; i += 64)
+            if (row0 + i < n_rows) reach.add(sight_of(a, (row0 + i) / c.group, true), true);
+    } else
+        reach.add(sight_of(a, 0, true), true);
+    const Walk walk = reach.walk<64>(a);
+    const int hi_last = reach.hi_last;
     const int64_t n_tiles = walk.count();
     const int t_begin = (int)(n_tiles * split / a.splits), t_end = (int)(n_tiles * (split + 1) / a.splits);
 
@@ -187,17 +164,7 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
                 bf16x8 weights[CT][2][NP];
 #pragma unroll
                 for (int i = 0; i < CT; ++i) {
-                    if (!whole) {
-                        if (tile * CACHE_TILE >= walk.sinks) {          // one run of keys
-                            const uint32_t at = j0 - see[i].from, span = see[i].last - see[i].from;
-                            const bool any = see[i].last >= see[i].from;
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) s[i][e] = any && at + 8 * (e / 4) + e % 4 <= span ? s[i][e] : -INFINITY;
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 16; ++e) s[i][e] = see[i].sees(j0 + 8 * (e / 4) + e % 4) ? s[i][e] : -INFINITY;
-                        }
-                    }
+                    if (!whole) see[i].hide(s[i], j0, tile, walk.sinks);
                     float top = -INFINITY;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
@@ -262,54 +229,18 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
     }
     if (!busy) return;
 
-    float *pt = part + ((size_t)a.part + (size_t)kvh * ((n_rows + ROWS - 1) / ROWS) * a.splits + unit) * cache_part_floats(ROWS, DP);    // (splits > 1)
-#pragma unroll
-    for (int i = 0; i < CT; ++i) {
-        l[i] += __shfl_xor(l[i], 32);
-        const int in_tile = 32 * CT * wave + 32 * i + col, row = row0 + in_tile;
-        if (a.splits > 1) {
-#pragma unroll
-            for (int f = 0; f < NW; ++f)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    *(float4 *)(pt + (size_t)in_tile * DP + 32 * f + 8 * e + 4 * half) = make_float4(acc[i][f][4 * e], acc[i][f][4 * e + 1], acc[i][f][4 * e + 2], acc[i][f][4 * e + 3]);
-            if (half == 0) pt[ROWS * DP + in_tile] = m[i], pt[ROWS * DP + ROWS + in_tile] = l[i];
-            continue;
-        }
-        if (row >= n_rows) continue;
-        const RowOf o = row_of(c, kvh, row);
-        const float over = l[i] == 0.f ? 0.f : 1.f / l[i];
-        char *out = a.out + (size_t)o.i * a.out_stride + (size_t)o.head * c.d_head * (DT == 0 ? 4 : 2);
-#pragma unroll
-        for (int f = 0; f < NW; ++f)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int at = 32 * f + 8 * e + 4 * half;
-                if (at >= c.d_head) continue;
-                float x[4];
-#pragma unroll
-                for (int y = 0; y < 4; ++y) x[y] = l[i] == 0.f ? 0.f : acc[i][f][4 * e + y] * over;
-                if (DT == 0) *(float4 *)(out + 4 * at) = make_float4(x[0], x[1], x[2], x[3]);
-                else *(uint2 *)(out + 2 * at) = make_uint2(f2bf(x[0]) | (uint32_t)f2bf(x[1]) << 16, f2bf(x[2]) | (uint32_t)f2bf(x[3]) << 16);
-            }
-        if (a.lse && half == 0) a.lse[(size_t)o.i * c.n_heads + o.head] = l[i] == 0.f ? -INFINITY : (m[i] + __builtin_amdgcn_logf(l[i])) * LN2;
-    }
+    finish_rows<DT, NW, CT, ROWS>(a, c, part, kvh, unit, n_rows, row0, 32 * CT * wave, col, half, acc, m, l);
 }
 
 template <int DT, int NW, int CT, int WAVES> void many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
     const dim3 grid(p.units, c.n_kv), block(64 * WAVES);
-    if constexpr (NW == 1)
-        if (c.d_head <= 16) {
-            hipLaunchKernelGGL((k_cache_many<DT, NW, CT, WAVES, 1>), grid, block, 0, s, args, dev, g, c, p.part);
-            return;
-        }
     hipLaunchKernelGGL((k_cache_many<DT, NW, CT, WAVES, 2 * NW>), grid, block, 0, s, args, dev, g, c, p.part);
 }
 template <int NW> void many_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
     if (c.dtype == 0) many<0, NW, 1, 4>(args, dev, g, c, p, s);
-    else if (NW <= 4 && p.rows_of_tile == 256) many<1, NW, NW <= 2 ? 1 : NW <= 4 ? 2 : 1, NW <= 2 ? 8 : 4>(args, dev, g, c, p, s);
+    else if (NW <= 4 && p.rows_of_tile == 256) many<1, NW, NW <= 4 ? 2 : 1, 4>(args, dev, g, c, p, s);
     else many<1, NW, 1, 4>(args, dev, g, c, p, s);
 }
 
@@ -318,8 +249,6 @@ template <int NW> void many_of(const CacheFew &args, const char *dev, const Cach
 void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
     switch (c.dp / 32) {
-    case 1: many_of<1>(args, dev, g, c, p, s); break;
-    case 2: many_of<2>(args, dev, g, c, p, s); break;
     case 3: many_of<3>(args, dev, g, c, p, s); break;
     case 4: many_of<4>(args, dev, g, c, p, s); break;
     case 5: many_of<5>(args, dev, g, c, p, s); break;
