@@ -10,7 +10,6 @@
 #include <algorithm>
 #include <cstdarg>
 #include <cstdio>
-#include <cstdlib>
 #include <exception>
 #include <new>
 #include <vector>
@@ -213,6 +212,12 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     s.d_head = f->d_head;
     s.dp = (f->d_head + CACHE_BLOCK - 1) / CACHE_BLOCK * CACHE_BLOCK;
     s.page_len = f->page_len;
+    // row / group with group <= 2^16: magic = ceil(2^(32 + shift) / group) with 2^shift < group <= 2^(shift + 1), whose error, below group <= 2^(shift + 1), times
+    // row < 2^31 stays below 2^(32 + shift)
+    if (s.group > 1) {
+        while ((2 << s.group_shift) < s.group) ++s.group_shift;
+        s.group_magic = (uint32_t)(((1ull << (32 + s.group_shift)) + s.group - 1) / s.group);
+    }
     const uint32_t tpp = f->page_len / CACHE_TILE;
     s.tpp_magic = tpp == 1 ? 0u : (uint32_t)(((1ull << 32) + tpp - 1) / tpp);
     s.dtype = f->dtype == AIF_F32 ? 0 : 1;
@@ -385,7 +390,13 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         for (int r = 0; r < n; ++r)
             if (mine(asks[r])) most = std::max(most, rows_of(asks[r])), wide += (rows_of(asks[r]) + 255) / 256 * sh.n_kv;
         if (most == 0) continue;
-        const int rows = p.rows_of_tile = kind ? (sh.dtype == 1 && sh.dp <= 128 && wide >= 2 * c->n_cu && !getenv("T128") ? 256 : 128) : (sh.dtype == 0 || most <= 16 ? 16 : 32);
+        const int rows = p.rows_of_tile = kind ? (sh.dtype == 1 && sh.dp <= 128 && wide >= 2 * c->n_cu ? 256 : 128) : (sh.dtype == 0 || most <= 16 ? 16 : 32);
+        // Heads of up to 32 features, and fp32 up to 64, are the cheapest to bring to bf16 once a wave (8 x 10^4 rows of 8 heads of 16 over 2,000 keys 255 us, 276
+        // once a block); up to 64 that also serves few row tiles, whose blocks wait for nobody, and rows that see each a window of its
+        // own, of which a wave's span less than a block's (replayed impressions 31 us, 48).
+        bool windows = false;
+        for (int r = 0; r < n; ++r) windows |= mine(asks[r]) && asks[r].pos && asks[r].window;
+        p.own = kind && sh.dp <= 64 && (sh.dp == 32 || sh.dtype == 0 || rows == 128 || windows);
         const int64_t room = (int64_t)c->n_cu * PART_ROWS / rows;
         auto tiles_of = [&](const CacheAsk &a) { return (rows_of(a) + rows - 1) / rows; };
         int64_t work = 0, units = 0, joined = 0, parts = 0;

@@ -19,6 +19,8 @@ struct CacheShape {
     int32_t *table;             // [max_seqs, pages_per_seq]: pages of each sequence, -1 = dropped
     size_t page_bytes;
     int32_t n_heads, n_kv, group, d_head, dp, page_len, pages_per_seq, dtype;
+    uint32_t group_magic;       // row / group for rows below 2^31: the high word of row * magic, shifted; 0: group is 1
+    int32_t group_shift;
     uint32_t tpp_magic;         // ceil(2^32 / tiles of a page): the high word of its product with a tile (< 2^27) is the tile's page; 0: one tile a page
     float scale;
 };
@@ -80,6 +82,7 @@ hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStr
 struct CachePart {
     int32_t units, joins;       // of all asks
     int32_t rows_of_tile;
+    bool own;                   // many rows: the kernel whose waves bring keys and values to bf16 for themselves
     float *part;                // partial results of split keys, a unit and kv head each: [rows][dp] sums, [rows] maxima, [rows] sums of weights
 };
 struct CachePlan {

@@ -50,24 +50,24 @@ __device__ __forceinline__ int ask_of(const char *dev, const CacheGrid &g, int u
 // What a row (query i and a head) sees: keys j <= last, and of those beyond `from` or before `sinks` only.
 struct Sight {
     int last, from, sinks;
-    __device__ __forceinline__ bool sees(int j) const { return j <= last && (j >= from || j < sinks); }
-    // scores of the keys j0 + 8 (e / 4) + e % 4 of a tile: minus infinity where not seen
-    __device__ __forceinline__ void hide(f32x16 &s, int j0, int tile, int all_sinks) const
+    __device__ __forceinline__ bool sees(int j) const { return (j <= last) & ((j >= from) | (j < sinks)); }
+    // scores of the keys j0 + 8 (e / 4) + e % 4: minus infinity where not seen (j0 = NO_KEY: everywhere)
+    __device__ __forceinline__ void hide(f32x16 &s, int j0) const
     {
-        if (tile * CACHE_TILE >= all_sinks) {               // one run of keys, [from, last]
-            const uint32_t at = (uint32_t)j0 - (uint32_t)from, span = last >= from ? last - from + 1 : 0;      // last - from < window
+        const uint32_t at = (uint32_t)j0 - (uint32_t)from, span = last >= from ? last - from + 1 : 0;      // last - from < window
+        const int head = min(sinks, last + 1);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = at + 8 * (e / 4) + e % 4 < span ? s[e] : -INFINITY;
-        } else {
-#pragma unroll
-            for (int e = 0; e < 16; ++e) s[e] = sees(j0 + 8 * (e / 4) + e % 4) ? s[e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) {
+            const int o = 8 * (e / 4) + e % 4;
+            s[e] = ((at + o < span) | (j0 + o < head)) ? s[e] : -INFINITY;
         }
     }
 };
+constexpr int NO_KEY = INT32_MAX - 2 * CACHE_TILE;
 __device__ __forceinline__ Sight sight_of(const CacheAsk &a, int i, bool is_row)
 {
     int p = a.len - 1;
-    if (a.pos && is_row) p = a.pos[i];
+    if (a.pos && is_row) p = as_global(a.pos)[i];
     p = is_row && p > -1 ? p : -1;
     Sight s;
     s.last = p < a.len - 1 ? p : a.len - 1;
@@ -191,14 +191,14 @@ template <int DT, int NP> __device__ __forceinline__ void query8(const char *q, 
 {
     if constexpr (DT == 1) {
         uint4 v = make_uint4(0, 0, 0, 0);
-        if (live && at < d) v = *(const uint4 *)(q + 2 * at);
+        if (live && at < d) v = *(const uint4 *)(as_global(q) + 2 * at);
         out[0] = __builtin_bit_cast(bf16x8, v);
     } else {
         float x[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (live && at + 4 * h < d) v = *(const float4 *)(q + 4 * (at + 4 * h));
+            if (live && at + 4 * h < d) v = *(const float4 *)(as_global(q) + 4 * (at + 4 * h));
             x[4 * h] = v.x, x[4 * h + 1] = v.y, x[4 * h + 2] = v.z, x[4 * h + 3] = v.w;
         }
         pieces8<NP>(x, out);
@@ -212,10 +212,21 @@ template <int DT, int NP> __device__ __forceinline__ void query8(const char *q, 
 struct RowOf {
     int i, head;
 };
-__device__ __forceinline__ RowOf row_of(const CacheShape &c, int kvh, int row) { return RowOf{row / c.group, kvh * c.group + row % c.group}; }
+__device__ __forceinline__ RowOf row_of(const CacheShape &c, int kvh, int row)
+{
+    const int i = c.group_magic ? (int)__umulhi((uint32_t)row, c.group_magic) >> c.group_shift : row;
+    return RowOf{i, kvh * c.group + row - i * c.group};
+}
 
-// Rows of values in LDS, whose parts are read four keys at a time: 64 bytes (modulo 128) apart, so that these lie in different banks.
-constexpr int v_stride(int dp) { return (2 * dp + 63) / 128 * 128 + 64; }
+// Values in LDS: rows of 2 dp bytes in pieces of 16, piece `at` of row `key` in the place of piece at ^ f(key), so that neither the eight rows whose pieces
+// are written together nor the four rows of which eight bytes a lane are read together meet in a bank.
+template <int DP> __device__ __forceinline__ int v_place(int key, int at) { return key * (2 * DP) + (at ^ (DP % 64 ? key / 2 % 4 : key % 8)) * 16; }
+// Where a lane's eight bytes of the turned read lie (four keys of one feature come back): keys key0 + lane % 16 / 4, 16 features from feature0 on
+// (both multiples of 4 and 16).
+template <int DP> __device__ __forceinline__ int v_turned(int key0, int feature0, int lane)
+{
+    return v_place<DP>(key0 + (lane & 15) / 4, feature0 / 8 + (lane & 3) / 2) + (lane & 1) * 8;
+}
 
 // The end of a wave's rows in_block + 32 i + col of a block's ROWS from `row0` on: quotients and logarithms, or a part for the join.  A lane holds
 // the features 32 f + 8 (e / 4) + 4 half + e % 4 of its row, and its own share of the sum l.

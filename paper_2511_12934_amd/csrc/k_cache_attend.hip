@@ -381,7 +381,7 @@ hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const
     for (int kind = 0; kind < 2; ++kind) {
         const CachePart &of = kind ? p.many : p.few;
         if (of.units == 0) continue;
-        if (kind && c.dp <= 64) launch_cache_own(args, asks.dev, g, c, of, s);
+        if (kind && of.own) launch_cache_own(args, asks.dev, g, c, of, s);
         else if (kind) launch_cache_many(args, asks.dev, g, c, of, s);
         else launch_cache_few(args, asks.dev, g, c, of, s);
         const hipError_t e = hipGetLastError();

@@ -1,12 +1,13 @@
-// The user cache's attention for many rows (candidates): a block takes 32 CT rows a wave, 4 waves, and 64 keys a stage.
+// The user cache's attention for many rows (candidates): a block takes 32 CT rows a wave, 4 or 8 waves, and 64 keys a stage.
 //
 // With hundreds of rows to a key the codes are the smaller part: a stage's keys and values are brought to bf16 once for the block, 32 features
 // and their scale a thread, and lie in LDS as rows; the next stage's codes travel meanwhile, and one barrier a stage parts the two
 // buffers.  Products are 32x32x16: S^T = K Q^T with a wave's queries in registers throughout, so that a lane holds 16 keys
 // of one row, and these, as weights, are the operand of O^T = V^T P^T as they stand; V comes turned (ds_read_b64_tr_b16).  What bounds it is
 // the vector ALU: per score one fused multiply-add, half a maximum, one exponential (2.3 times a plain instruction), half a conversion and one
-// addition.
-// Rows of K are 16 bytes longer than their features, rows of V 64 (modulo 128): the lanes of a read meet different banks.
+// addition.  Heads of 64: eight waves of 32 rows, four waves a SIMD (64 x 10^4 rows over 500 keys 124 us; four waves of 64 rows 137 with waves on their
+// own, k_cache_own).
+// Rows of K are 16 bytes longer than their features: the lanes of a read meet different banks (V: v_place).
 #include "k_cache_attend.h"
 
 namespace aif {
@@ -15,11 +16,11 @@ namespace {
 
 
 constexpr int k_stride(int dp) { return 2 * dp + 16; }
-constexpr int stage_bytes(int dp) { return 2 * CACHE_TILE * (k_stride(dp) + v_stride(dp)); }
+constexpr int stage_bytes(int dp) { return 2 * CACHE_TILE * (k_stride(dp) + 2 * dp); }
 
-template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? (NW <= 2 ? 4 : 2) : NW <= 2 ? 2 : 1) void k_cache_many(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
+template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds__(64 * WAVES, WAVES == 8 ? 4 : 1) void k_cache_many(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
 {
-    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 32 * WAVES * CT, THREADS = 64 * WAVES, KST = k_stride(DP), VST = v_stride(DP);
+    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 32 * WAVES * CT, THREADS = 64 * WAVES, KST = k_stride(DP);
     constexpr int ITEMS = (128 * NW + THREADS - 1) / THREADS;       // pieces of 32 features a thread brings to LDS per stage
     __shared__ __align__(16) char lds[2][stage_bytes(DP)];
     __shared__ int odd_now[3];                          // whether a stage has blocks of values that are not finite
@@ -27,10 +28,15 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5, kvh = blockIdx.y;
     const int r = ask_of(dev, g, blockIdx.x, lane);
     const CacheAsk a = ask_at(dev, r);
-    const int unit = (int)blockIdx.x - first_at(dev, g, r), row_tile = unit / a.splits, split = unit % a.splits;
-    const int n_rows = a.n_q * c.group, row0 = row_tile * ROWS;
+    const int unit = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group;
+    int row_tile = unit, split = 0;
+    if (a.splits > 1) row_tile = unit / a.splits, split = unit % a.splits;
+    const char *pool = as_global(c.pool) + (size_t)kvh * cache_head_bytes(c);
+    const float k2 = c.scale * LOG2E;
+    typedef s16x4 __attribute__((address_space(3))) *lds4_t;
+    const int row0 = row_tile * ROWS;
 
-    // every wave looks over all the block's rows, for the walk; its own are [row0 + 32 CT wave, + 32 CT)
+
     Reach reach;
     if (a.pos) {
         for (int i = lane; i < ROWS; i += 64)
@@ -39,10 +45,12 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
         reach.add(sight_of(a, 0, true), true);
     const Walk walk = reach.walk<64>(a);
     const int hi_last = reach.hi_last;
-    const int64_t n_tiles = walk.count();
-    const int t_begin = (int)(n_tiles * split / a.splits), t_end = (int)(n_tiles * (split + 1) / a.splits);
-
-    const char *pool = c.pool + (size_t)kvh * cache_head_bytes(c);
+    int t_begin = 0, t_end = walk.count();
+    if (a.splits > 1) {
+        const int64_t n = t_end;
+        t_begin = (int)(n * split / a.splits);
+        t_end = (int)(n * (split + 1) / a.splits);
+    }
     TileList<DP> list;
     list.fill(c, a, walk, t_begin, 1, t_end, lane);
     // tile t of the walk (t - list.from in 0..63); dead: behind the end, or in a page that was dropped.  A dead tile reads
@@ -83,11 +91,10 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
                 sc = fine ? sc : 1.f;
                 raw[i].x = fine ? raw[i].x : 0u, raw[i].y = fine ? raw[i].y : 0u, raw[i].z = fine ? raw[i].z : 0u, raw[i].w = fine ? raw[i].w : 0u;
             }
-            bf16x8 *to = (bf16x8 *)(lds[buf] + (vals ? 2 * CACHE_TILE * KST + (tile * CACHE_TILE + row) * VST : (tile * CACHE_TILE + row) * KST) + blk * 64);
-            to[0] = decode8(raw[i].x, sc);
-            to[1] = decode8(raw[i].y, sc);
-            to[2] = decode8(raw[i].z, sc);
-            to[3] = decode8(raw[i].w, sc);
+            char *keys = lds[buf] + (tile * CACHE_TILE + row) * KST + blk * 64, *turn = lds[buf] + 2 * CACHE_TILE * (KST + tile * DP);
+            const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
+#pragma unroll
+            for (int x = 0; x < 4; ++x) *(bf16x8 *)(vals ? turn + v_place<DP>(row, 4 * blk + x) : keys + 16 * x) = decode8(w[x], sc);
         }
         if (odd) odd_now[flag] = 1;
     };
@@ -122,9 +129,6 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[t][f][e] = 0.f;
     }
-    const float k2 = c.scale * LOG2E;
-    typedef s16x4 __attribute__((address_space(3))) *lds4_t;
-
     if (threadIdx.x < 3) odd_now[threadIdx.x] = 0;
     if (t_begin < t_end) {
     bool dead0, dead1;
@@ -164,7 +168,7 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
                 bf16x8 weights[CT][2][NP];
 #pragma unroll
                 for (int i = 0; i < CT; ++i) {
-                    if (!whole) see[i].hide(s[i], j0, tile, walk.sinks);
+                    if (!whole) see[i].hide(s[i], j0);
                     float top = -INFINITY;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
@@ -192,13 +196,14 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
 #pragma unroll
                     for (int f = 0; f < NW; ++f) {
                         // four keys of 16 features a group of 16 lanes: keys 16 k + 4 half (+ 8), features 32 f + 16 (lane / 16 % 2)
-                        const char *from = vb + (h * CACHE_TILE + 16 * k + 4 * half + (lane & 15) / 4) * VST + 64 * f + 32 * (lane >> 4 & 1) + (lane & 3) * 8;
+                        const char *turn = vb + h * CACHE_TILE * 2 * DP;
+                        const int key = 16 * k + 4 * half, feature = 32 * f + 16 * (lane >> 4 & 1);
                         union {
                             s16x4 h[2];
                             bf16x8 all;
                         } v;
-                        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)from);
-                        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(from + 8 * VST));
+                        v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turn + v_turned<DP>(key, feature, lane)));
+                        v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turn + v_turned<DP>(key + 8, feature, lane)));
 #pragma unroll
                         for (int i = 0; i < CT; ++i)
 #pragma unroll
@@ -227,9 +232,7 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
         __syncthreads();
     }
     }
-    if (!busy) return;
-
-    finish_rows<DT, NW, CT, ROWS>(a, c, part, kvh, unit, n_rows, row0, 32 * CT * wave, col, half, acc, m, l);
+    if (busy) finish_rows<DT, NW, CT, ROWS>(a, c, part, kvh, unit, n_rows, row0, 32 * CT * wave, col, half, acc, m, l);
 }
 
 template <int DT, int NW, int CT, int WAVES> void many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
@@ -239,7 +242,8 @@ template <int DT, int NW, int CT, int WAVES> void many(const CacheFew &args, con
 }
 template <int NW> void many_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
-    if (c.dtype == 0) many<0, NW, 1, 4>(args, dev, g, c, p, s);
+    if constexpr (NW == 2) many<1, NW, 1, 8>(args, dev, g, c, p, s);
+    else if (c.dtype == 0) many<0, NW, 1, 4>(args, dev, g, c, p, s);
     else if (NW <= 4 && p.rows_of_tile == 256) many<1, NW, NW <= 4 ? 2 : 1, 4>(args, dev, g, c, p, s);
     else many<1, NW, 1, 4>(args, dev, g, c, p, s);
 }
@@ -249,6 +253,7 @@ template <int NW> void many_of(const CacheFew &args, const char *dev, const Cach
 void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
     switch (c.dp / 32) {
+    case 2: many_of<2>(args, dev, g, c, p, s); break;
     case 3: many_of<3>(args, dev, g, c, p, s); break;
     case 4: many_of<4>(args, dev, g, c, p, s); break;
     case 5: many_of<5>(args, dev, g, c, p, s); break;

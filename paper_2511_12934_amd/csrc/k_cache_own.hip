@@ -13,17 +13,22 @@ namespace {
 
 template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) void k_cache_own(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
 {
-    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 128 * CT, VST = v_stride(DP);
-    __shared__ __align__(16) char lds[4][CACHE_TILE * VST];
+    constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 128 * CT;
+    __shared__ __align__(16) char lds[4][CACHE_TILE * 2 * DP];
     (void)few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5, kvh = blockIdx.y;
     const int r = ask_of(dev, g, blockIdx.x, lane);
     const CacheAsk a = ask_at(dev, r);
-    int row_tile = (int)blockIdx.x - first_at(dev, g, r), split = 0;
-    const int unit = row_tile;
+    const int unit = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group, in_block = 32 * CT * wave;
+    int row_tile = unit, split = 0;
     if (a.splits > 1) row_tile = unit / a.splits, split = unit % a.splits;
-    const int n_rows = a.n_q * c.group, in_block = 32 * CT * wave, row0 = row_tile * ROWS + in_block;
+    const char *pool = as_global(c.pool) + (size_t)kvh * cache_head_bytes(c);
+    const float k2 = c.scale * LOG2E;
+    typedef s16x4 __attribute__((address_space(3))) *lds4_t;
+    char *mine = lds[wave];
+    const int row0 = row_tile * ROWS + in_block;
     if (row0 >= n_rows) return;                 // no wave waits for another
+
 
     Sight see[CT];
     bf16x8 q[CT][NP][KS];
@@ -62,21 +67,14 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
 #pragma unroll
             for (int e = 0; e < 16; ++e) acc[i][f][e] = 0.f;
     }
-    const float k2 = c.scale * LOG2E;
-    typedef s16x4 __attribute__((address_space(3))) *lds4_t;
-    char *mine = lds[wave];
-    // four keys of 16 features a group of 16 lanes
-    const char *turned = mine + (4 * half + (lane & 15) / 4) * VST + 32 * (lane >> 4 & 1) + (lane & 3) * 8;
-
-    const char *pool = as_global(c.pool) + (size_t)kvh * cache_head_bytes(c);
     TileList<DP> list;
     list.fill(c, a, walk, t, 1, t_end, lane);
     struct Raw {
-        uint32_t k[KS], v[KS], ks, vs;             // words of eight codes: features half 8 KS on, of a key
+        uint32_t k[KS], v[KS], ks, vs;          // words of eight codes: features half 8 KS on, of a key
         bool here;
     };
     const uint32_t word_at = col * (DP / 2) + half * (4 * KS), byte_at = col * NW + (NW == 2 ? half : 0);
-    auto ask = [&](int t, Raw &raw) {           // a tile that is dropped or behind the end reads page 0
+    auto ask = [&](int t, Raw &raw) {           // a tile that is dropped or behind the end reads page 0, which nobody sees
         if (t - list.from == 64) list.fill(c, a, walk, t, 1, t_end, lane);
         const int64_t off = list.offset(t - list.from);
         const char *tile = pool + (off < 0 ? 0 : off);
@@ -86,62 +84,76 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
         raw.vs = *(const uint8_t *)(tile + 33 * DP + byte_at);
         raw.here = off >= 0;
     };
-    auto work = [&](int t, Raw &now) {
-        if (!now.here) return;
-        asm volatile("" : "+v"(now.ks), "+v"(now.vs));      // (made use of here, not where they are asked for)
-        const int tile = walk.tile(t), j0 = tile * CACHE_TILE + 4 * half;
 
-        f32x16 s[CT];
+    bf16x8 kf[KS], vf[2][NW];
+    // The first product of row tile o of a tile whose keys kf holds, or, `fresh`, has yet to hold: step k of it.
+    auto scores = [&](int o, int k, f32x16 &so) {
+        if (k == 0)
 #pragma unroll
-        for (int i = 0; i < CT; ++i)
+            for (int e = 0; e < 16; ++e) so[e] = 0.f;
 #pragma unroll
-            for (int e = 0; e < 16; ++e) s[i][e] = 0.f;
-        const float ks = scale_of(now.ks);
+        for (int p = NP - 1; p >= 0; --p) so = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k], q[o][p][k], so, 0, 0, 0);
+    };
+    // One phase: the weights of row tile i from its scores si beside the scores so of row tile o, then their product with the values.
+    // fresh: the keys for so are those of `keys`, from here on.
+    auto phase = [&](int i, f32x16 &si, int o, f32x16 &so, bool fresh, const Raw &keys, int tile, bool here) {
+        if (!here || !walk.whole(tile)) see[i].hide(si, here ? tile * CACHE_TILE + 4 * half : NO_KEY);
+        float top = -INFINITY;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) top = fmaxf(top, si[e]);
+        top *= k2;
+        if (__ballot(top > m[i] + LAZY)) {
+            top = fmaxf(top, __shfl_xor(top, 32));
+            const float m2 = fmaxf(m[i], top);
+            if (__ballot(m[i] != -INFINITY)) {
+                const float back = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - m2);
+                l[i] *= back;
+#pragma unroll
+                for (int f = 0; f < NW; ++f) acc[i][f] *= back;
+            }
+            m[i] = m2;
+        }
+        const float ref = m[i] == -INFINITY ? 0.f : m[i];
+        const float ks = scale_of(keys.ks);
+        float x[16];
+        constexpr int EACH = 16 / KS;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
-            const bf16x8 kf = decode8(now.k[k], ks);
+            if (fresh) kf[k] = decode8(keys.k[k], ks);
+            scores(o, k, so);
 #pragma unroll
-            for (int i = 0; i < CT; ++i)
-#pragma unroll
-                for (int p = NP - 1; p >= 0; --p) s[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf, q[i][p][k], s[i], 0, 0, 0);
+            for (int e = EACH * k; e < EACH * (k + 1); ++e) x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(si[e], k2, -ref));
+            __builtin_amdgcn_sched_barrier(0);
         }
+        bf16x8 weights[2][NP];
+        pieces8<NP>(x, weights[0]);
+        pieces8<NP>(x + 8, weights[1]);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int f = 0; f < NW; ++f) {
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p) acc[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[k][f], weights[k][p], acc[i][f], 0, 0, 0);
+#pragma unroll
+                for (int e = 8 * k + 8 / NW * f; e < 8 * k + 8 / NW * (f + 1); ++e) l[i] += x[e];
+                __builtin_amdgcn_sched_barrier(0);
+            }
+    };
+    // Tile t: its scores s0 (of row tile 0) are there, kf holds its keys where CT = 2, and `next` the codes of the tile behind it,
+    // whose scores s1 (CT = 1; of row tile 0 again: s0) are there in the end.
+    auto step = [&](int t, Raw &now, Raw &next, f32x16 &s0, f32x16 &s1) {
+        asm volatile("" : "+v"(now.vs), "+v"(next.ks));     // (made use of here, not where they are asked for)
+        const int tile = walk.tile(t);
+        const bool here = now.here;
         // a block of values that is not finite becomes zeros: who sees it gets NaN below
         float vs = scale_of(now.vs);
         const bool fine = vs < 0x1p126f;
         vs = fine ? vs : 1.f;
 #pragma unroll
-        for (int w = 0; w < KS; ++w) *(bf16x8 *)(mine + col * VST + (half * KS + w) * 16) = decode8(fine ? now.v[w] : 0u, vs);
-
-        const bool whole = walk.whole(tile);
-        bf16x8 weights[CT][2][NP];
-#pragma unroll
-        for (int i = 0; i < CT; ++i) {
-            if (!whole) see[i].hide(s[i], j0, tile, walk.sinks);
-            float top = -INFINITY;
-#pragma unroll
-            for (int e = 0; e < 16; ++e) top = fmaxf(top, s[i][e]);
-            top *= k2;
-            if (__ballot(top > m[i] + LAZY)) {
-                top = fmaxf(top, __shfl_xor(top, 32));
-                const float m2 = fmaxf(m[i], top);
-                if (__ballot(m[i] != -INFINITY)) {
-                    const float back = m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[i] - m2);
-                    l[i] *= back;
-#pragma unroll
-                    for (int f = 0; f < NW; ++f) acc[i][f] *= back;
-                }
-                m[i] = m2;
-            }
-            const float ref = m[i] == -INFINITY ? 0.f : m[i];
-            float x[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[i][e], k2, -ref));
-                l[i] += x[e];
-            }
-            pieces8<NP>(x, weights[i][0]);
-            pieces8<NP>(x + 8, weights[i][1]);
-        }
+        for (int w = 0; w < KS; ++w) *(bf16x8 *)(mine + v_place<DP>(col, half * KS + w)) = decode8(fine ? now.v[w] : 0u, vs);
+        ask(t + 2, now);
 #pragma unroll
         for (int k = 0; k < 2; ++k)
 #pragma unroll
@@ -150,14 +162,17 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
                     s16x4 h[2];
                     bf16x8 all;
                 } v;
-                v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turned + 16 * k * VST + 64 * f));
-                v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turned + (16 * k + 8) * VST + 64 * f));
-#pragma unroll
-                for (int i = 0; i < CT; ++i)
-#pragma unroll
-                    for (int p = NP - 1; p >= 0; --p) acc[i][f] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v.all, weights[i][k][p], acc[i][f], 0, 0, 0);
+                const int key = 16 * k + 4 * half, feature = 32 * f + 16 * (lane >> 4 & 1);
+                v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(mine + v_turned<DP>(key, feature, lane)));
+                v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(mine + v_turned<DP>(key + 8, feature, lane)));
+                vf[k][f] = v.all;
             }
-        if (__ballot(!fine && tile * CACHE_TILE + col <= reach.hi_last)) {
+        if constexpr (CT == 2) {
+            phase(0, s0, 1, s1, false, next, tile, here);
+            phase(1, s1, 0, s0, true, next, tile, here);
+        } else
+            phase(0, s0, 0, s1, true, next, tile, here);
+        if (__ballot(!fine && here && tile * CACHE_TILE + col <= reach.hi_last)) {
             // a row that sees a block of values that is not finite: its features are NaN
 #pragma unroll 1
             for (int key = 0; key < CACHE_TILE; ++key)
@@ -172,14 +187,25 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
     };
     // two sets of registers by turns: what one is loaded with is not waited for while the other is worked on
     Raw raw0, raw1;
+    f32x16 s0, s1;
     ask(t, raw0);
-    for (; t < t_end; t += 2) {
-        ask(t + 1, raw1);
-        work(t, raw0);
-        ask(t + 2, raw0);
-        if (t + 1 < t_end) work(t + 1, raw1);
+    ask(t + 1, raw1);
+    asm volatile("" : "+v"(raw0.ks));
+#pragma unroll
+    for (int k = 0; k < KS; ++k) {
+        kf[k] = decode8(raw0.k[k], scale_of(raw0.ks));
+        scores(0, k, s0);
     }
-    finish_rows<DT, NW, CT, ROWS>(a, c, part, kvh, unit, n_rows, row_tile * ROWS, in_block, col, half, acc, m, l);
+    for (; t < t_end; t += 2) {
+        if constexpr (CT == 2) {
+            step(t, raw0, raw1, s0, s1);
+            step(t + 1, raw1, raw0, s0, s1);
+        } else {
+            step(t, raw0, raw1, s0, s1);
+            step(t + 1, raw1, raw0, s1, s0);
+        }
+    }
+    finish_rows<DT, NW, CT, ROWS>(a, c, part, kvh, unit, n_rows, row0 - in_block, in_block, col, half, acc, m, l);
 }
 
 template <int DT, int NW, int CT> void own(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
