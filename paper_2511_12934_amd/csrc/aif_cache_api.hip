@@ -18,8 +18,8 @@ using namespace aif;
 
 namespace {
 constexpr int CACHE_NSLOT = 8;
-constexpr size_t CACHE_SLOT_BYTES = 64 << 10;
-constexpr int FEW_ROWS = 64, MIN_TILES = 8, MAX_SPLITS = 128, PART_ROWS = 256;     // plan_attend
+constexpr size_t CACHE_SLOT_BYTES = 512 << 10;
+constexpr int FEW_ROWS = 64, MIN_TILES = 8, MAX_SPLITS = 128, PART_ROWS = 384;     // plan_attend
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
 }  // namespace
@@ -129,7 +129,7 @@ aif_status check_stream(aif_cache_ctx *c, hipStream_t s)
 }
 
 // A list of descriptors on its way to a launch.  Up to CACHE_FEW_BYTES of a call travel in the kernel's arguments; more are
-// cut into lists of a slot of the pinned ring each, uploaded on the stream.
+// cut into lists of a slot of the pinned ring each.
 template <class T> class CacheBatch {
 public:
     CacheBatch(aif_cache_ctx *c, size_t expected, hipStream_t s) : c_(c), s_(s), far_(expected * sizeof(T) > CACHE_FEW_BYTES) {}
@@ -160,9 +160,10 @@ public:
         CacheList l{at_, nullptr, n_, (size_t)n_ * sizeof(T)};
         n_ = 0;
         if (far_) {
+            // a descriptor is read by one block, or one a head: from the pinned memory itself where that is mapped
             const size_t off = (size_t)slot_ * c_->slot_bytes;
-            CACHE_TRY(c_, staging_upload(c_->h_stage, c_->h_stage_dev, off, c_->d_stage + off, l.bytes, s_));
-            l.dev = c_->d_stage + off;
+            l.dev = c_->h_stage_dev ? c_->h_stage_dev + off : c_->d_stage + off;
+            if (!c_->h_stage_dev) CACHE_TRY(c_, staging_upload(c_->h_stage, nullptr, off, c_->d_stage + off, l.bytes, s_));
         }
         CACHE_TRY(c_, go(l));
         if (far_) {
@@ -372,7 +373,8 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
 // (fp32: 16, a query's three pieces take the registers), the others to the one whose tiles are 128 or, bf16 heads of up to 128 and
 // enough of them, 256.  Where the (row tile, kv head) pairs are fewer than the device holds blocks, their keys are shared
 // out as well, in splits of at least MIN_TILES tiles of 32 keys, so that a split outlasts its start.  Partial results have room for
-// PART_ROWS rows a compute unit and kernel: tiles * splits <= tiles * keys / chunk <= work / chunk <= room.
+// PART_ROWS rows a compute unit and kernel: keys / chunk is rounded, by a third up at most where that makes two or more, and
+// tiles * keys / chunk <= work / chunk <= 3 / 4 of the room.
 static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays, CachePlan &plan, size_t &bytes)
 {
     const CacheShape &sh = c->shape;
@@ -402,7 +404,7 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         int64_t work = 0, units = 0, joined = 0, parts = 0;
         for (int r = 0; r < n; ++r)
             if (mine(asks[r])) work += tiles_of(asks[r]) * keys_of(asks[r]) * sh.n_kv;
-        const int64_t blocks = std::min<int64_t>(room, (int64_t)c->n_cu * (kind ? 2 : 4));
+        const int64_t blocks = std::min<int64_t>(room * 3 / 4, (int64_t)c->n_cu * (kind || sh.dp > 64 ? 2 : 4));      // a compute unit holds about so many
         const int64_t chunk = std::max<int64_t>(MIN_TILES, (work + blocks - 1) / blocks);
         int32_t *first = arrays, *joins = arrays + n + 1;
         arrays += 2 * (n + 1);
@@ -413,7 +415,7 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
             joins[r] = (int32_t)joined;
             if (!mine(a)) continue;
             const int64_t tiles = tiles_of(a);
-            a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, keys_of(a) / chunk), MAX_SPLITS);
+            a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, (keys_of(a) + chunk / 2) / chunk), MAX_SPLITS);
             a.part = (int32_t)parts;
             units += tiles * a.splits;
             if (a.splits > 1) {

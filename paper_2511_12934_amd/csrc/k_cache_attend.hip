@@ -245,15 +245,18 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
             }
         }
     };
-    // two sets of registers by turns: what one is loaded with is not waited for while the other is worked on
-    RawTile<NW> raw0, raw1;
-    ask(t, raw0);
-    for (; t < t_end; t += 8) {
-        ask(t + 4, raw1);
-        work(t, raw0);
-        ask(t + 8, raw0);
-        if (t + 4 < t_end) work(t + 4, raw1);
-    }
+    // Sets of registers by turns: what one is loaded with is not waited for while another is worked on.  A wave of a short call has few tiles,
+    // and its time is that of the loads behind one another: all it can hold are on their way at once.
+    constexpr int DEPTH = DT == 1 && NT == 1 && NW <= 4 ? 4 : 2;
+    RawTile<NW> raw[DEPTH];
+#pragma unroll
+    for (int i = 0; i < DEPTH - 1; ++i) ask(t + 4 * i, raw[i]);
+    for (; t < t_end; t += 4 * DEPTH)
+#pragma unroll
+        for (int i = 0; i < DEPTH; ++i) {
+            ask(t + 4 * (i + DEPTH - 1), raw[(i + DEPTH - 1) % DEPTH]);
+            if (t + 4 * i < t_end) work(t + 4 * i, raw[i]);
+        }
 
     // the four waves' parts become one: a common reference, then sums through LDS
 #pragma unroll
@@ -315,23 +318,42 @@ template <int DT> __global__ __launch_bounds__(128) void k_cache_join(CacheFew f
     const CacheAsk a = ask_at(dev, r);
     const int row = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group, tiles = (n_rows + rows_of_tile - 1) / rows_of_tile;
     const size_t each = cache_part_floats(rows_of_tile, c.dp);
-    const float *p = part + ((size_t)a.part + ((size_t)kvh * tiles + row / rows_of_tile) * a.splits) * each;
+    const float *p = as_global(part) + ((size_t)a.part + ((size_t)kvh * tiles + row / rows_of_tile) * a.splits) * each;
     const int cl = row % rows_of_tile;
     const float *ms = p + (size_t)rows_of_tile * c.dp + cl, *ls = ms + rows_of_tile;
-    float mt = -INFINITY;
-    for (int s = lane; s < a.splits; s += 64) mt = fmaxf(mt, ms[s * each]);
+    // a lane to a split for what its part counts; MAX_SPLITS is 128
+    __shared__ float back[128];
+    float mw[2], lw[2], mt = -INFINITY;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int s = lane + 64 * h;
+        mw[h] = s < a.splits ? ms[s * each] : -INFINITY;
+        lw[h] = s < a.splits ? ls[s * each] : 0.f;
+        mt = fmaxf(mt, mw[h]);
+    }
     for (int x = 1; x < 64; x *= 2) mt = fmaxf(mt, __shfl_xor(mt, x));
+    float sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float w = mw[h] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw[h] - mt);      // without a maximum: zeros, or NaN
+        if (threadIdx.x < 64) back[lane + 64 * h] = w;
+        sum += lw[h] * w;
+    }
+    for (int x = 1; x < 64; x *= 2) sum += __shfl_xor(sum, x);
+    __syncthreads();
     const RowOf at = row_of(c, kvh, row);
-    float sum = 0.f, o[2] = {0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const float mw = ms[s * each], back = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mw - mt);     // without a maximum: zeros, or NaN
-        sum += ls[s * each] * back;
+    float o[2] = {0.f, 0.f};
+    for (int s = 0; s < a.splits; s += 8)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int f = threadIdx.x + 128 * h;
-            if (f < c.dp) o[h] += p[s * each + (size_t)cl * c.dp + f] * back;
+            if (f >= c.dp) break;
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = p[(size_t)min(s + i, a.splits - 1) * each + (size_t)cl * c.dp + f];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[h] += s + i < a.splits ? x[i] * back[s + i] : 0.f;
         }
-    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
         const int f = threadIdx.x + 128 * h;

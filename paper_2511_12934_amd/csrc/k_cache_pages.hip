@@ -7,7 +7,7 @@ namespace aif {
 
 namespace {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 // features [at, at + 8) of a row of d features, zeros past its end
 template <int DT> __device__ __forceinline__ void load8(const char *row, int at, int d, float *x)
@@ -25,33 +25,6 @@ template <int DT> __device__ __forceinline__ void load8(const char *row, int at,
         const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[2 * i] = __uint_as_float(w[i] << 16), x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-}
-
-template <int DT> __device__ __forceinline__ void store8(char *row, int at, int d, uint32_t codes, float scale)
-{
-    if constexpr (DT == 0) {
-        float x[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            bf16x2 v;
-            if (i == 0) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0);
-            if (i == 1) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);
-            if (i == 2) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2);
-            if (i == 3) v = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
-            const uint32_t w = __builtin_bit_cast(uint32_t, v);
-            x[2 * i] = __uint_as_float(w << 16), x[2 * i + 1] = __uint_as_float(w & 0xffff0000u);
-        }
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            if (at + 4 * h < d) *(float4 *)(row + 4 * (at + 4 * h)) = make_float4(x[4 * h], x[4 * h + 1], x[4 * h + 2], x[4 * h + 3]);
-    } else if (at < d) {
-        uint4 v;
-        v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0));
-        v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1));
-        v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2));
-        v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3));
-        *(uint4 *)(row + 2 * at) = v;
     }
 }
 
@@ -99,7 +72,7 @@ template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_app
 {
     const CacheUnit u = cache_desc<CacheUnit>(list, (size_t)blockIdx.x * sizeof(CacheUnit));
     const int head = blockIdx.y, dp = c.dp, per_row = dp / 8, esz = DT == 0 ? 4 : 2;
-    char *page = c.pool + (size_t)u.page * c.page_bytes + (size_t)head * cache_head_bytes(c);
+    char *page = as_global(c.pool) + (size_t)u.page * c.page_bytes + (size_t)head * cache_head_bytes(c);
     if (threadIdx.x == 0 && head == 0) c.table[u.entry] = u.page;
     if (u.cow >= 0) {
         const char *from = c.pool + (size_t)u.cow * c.page_bytes + (size_t)head * cache_head_bytes(c);
@@ -118,36 +91,66 @@ template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_app
             b.scales[dp + at] = a.scales[dp + at];
         }
     }
-    for (int i = threadIdx.x; i < 2 * u.n * per_row; i += 256) {
-        const int half = i >= u.n * per_row, j = half ? i - u.n * per_row : i;
-        const int row = j / per_row, at = j % per_row * 8;
-        const char *src = (half ? u.vals + (size_t)row * u.val_stride * esz : u.keys + (size_t)row * u.key_stride * esz) + (size_t)head * c.d_head * esz;
-        float x[8];
-        load8<DT>(src, at, c.d_head, x);
-        uint32_t byte;
-        const uint32_t codes = encode8(x, byte);
-        const RowAt to = row_at(page, dp, u.row0 + row);
-        *(uint32_t *)(to.codes + (half ? 16 * dp : 0) + at / 2) = codes;
-        if (at % CACHE_BLOCK == 0) to.scales[(half ? dp : 0) + at / CACHE_BLOCK] = (char)byte;
+    // a thread keeps its features; two rows' keys and values are asked for before the first is worked on
+    const int step = 256 / per_row, at = threadIdx.x % per_row * 8;
+    const char *keys = as_global(u.keys) + (size_t)head * c.d_head * esz, *vals = as_global(u.vals) + (size_t)head * c.d_head * esz;
+    for (int row = threadIdx.x / per_row; row < u.n && threadIdx.x < step * per_row; row += 2 * step) {
+        float x[4][8];
+        const bool two = row + step < u.n;
+        load8<DT>(keys + (size_t)row * u.key_stride * esz, at, c.d_head, x[0]);
+        load8<DT>(vals + (size_t)row * u.val_stride * esz, at, c.d_head, x[1]);
+        load8<DT>(keys + (size_t)(two ? row + step : row) * u.key_stride * esz, at, c.d_head, x[2]);
+        load8<DT>(vals + (size_t)(two ? row + step : row) * u.val_stride * esz, at, c.d_head, x[3]);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (i >= 2 && !two) break;
+            uint32_t byte;
+            const uint32_t codes = encode8(x[i], byte);
+            const RowAt to = row_at(page, dp, u.row0 + row + (i >= 2 ? step : 0));
+            *(uint32_t *)(to.codes + (i & 1 ? 16 * dp : 0) + at / 2) = codes;
+            if (at % CACHE_BLOCK == 0) to.scales[(i & 1 ? dp : 0) + at / CACHE_BLOCK] = (char)byte;
+        }
     }
 }
 
-// The way back: rows of a page to keys and vals (null: not wanted), which are written.
+// The way back: rows of a page to keys and vals (null: not wanted), which are written.  A thread takes 16 bytes of them, so that neighbours'
+// pieces make whole lines (fp32 in pieces of 32 bytes: 378 us for what takes READ_LONG).
 template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_read(ARGS list, CacheShape c)
 {
+    constexpr int WIDE = DT == 0 ? 4 : 8, ESZ = DT == 0 ? 4 : 2;
     const CacheUnit u = cache_desc<CacheUnit>(list, (size_t)blockIdx.x * sizeof(CacheUnit));
-    const int head = blockIdx.y, dp = c.dp, per_row = dp / 8, esz = DT == 0 ? 4 : 2;
-    char *page = c.pool + (size_t)u.page * c.page_bytes + (size_t)head * cache_head_bytes(c);
-    for (int i = threadIdx.x; i < 2 * u.n * per_row; i += 256) {
-        const int half = i >= u.n * per_row, j = half ? i - u.n * per_row : i;
-        const int row = j / per_row, at = j % per_row * 8;
-        char *dst = const_cast<char *>(half ? u.vals : u.keys);
-        if (!dst) continue;
-        dst += (size_t)row * (half ? u.val_stride : u.key_stride) * esz + (size_t)head * c.d_head * esz;
-        const RowAt from = row_at(page, dp, u.row0 + row);
-        const uint32_t codes = *(const uint32_t *)(from.codes + (half ? 16 * dp : 0) + at / 2);
-        const uint32_t byte = (uint8_t)from.scales[(half ? dp : 0) + at / CACHE_BLOCK];
-        store8<DT>(dst, at, c.d_head, codes, __uint_as_float(byte << 23));
+    const int head = blockIdx.y, dp = c.dp, per_row = dp / WIDE;
+    char *page = as_global(c.pool) + (size_t)u.page * c.page_bytes + (size_t)head * cache_head_bytes(c);
+    const int step = 256 / per_row, at = threadIdx.x % per_row * WIDE;
+    char *keys = const_cast<char *>(as_global(u.keys)), *vals = const_cast<char *>(as_global(u.vals));
+    if (at >= c.d_head) return;
+    for (int row = threadIdx.x / per_row; row < u.n && threadIdx.x < step * per_row; row += 4 * step) {
+        uint32_t codes[8], byte[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row + i / 2 * step;
+            const RowAt from = row_at(page, dp, u.row0 + (r < u.n ? r : row));
+            const char *p = from.codes + (i & 1 ? 16 * dp : 0) + at / 2;
+            codes[i] = DT == 0 ? *(const uint16_t *)p : *(const uint32_t *)p;
+            byte[i] = (uint8_t)from.scales[(i & 1 ? dp : 0) + at / CACHE_BLOCK];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = row + i / 2 * step;
+            char *dst = i & 1 ? vals : keys;
+            if (r >= u.n || !dst) continue;
+            const float scale = __uint_as_float(byte[i] << 23);
+            u32x4 v;
+            v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 0));
+            v.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 1));
+            if constexpr (DT == 0) {
+                v = u32x4{v.x << 16, v.x & 0xffff0000u, v.y << 16, v.y & 0xffff0000u};
+            } else {
+                v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 2));
+                v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 3));
+            }
+            __builtin_nontemporal_store(v, (u32x4 *)(dst + ((size_t)r * (i & 1 ? u.val_stride : u.key_stride) + (size_t)head * c.d_head + at) * ESZ));
+        }
     }
 }
 
@@ -158,23 +161,24 @@ template <class ARGS> __global__ __launch_bounds__(256) void k_cache_fill(ARGS l
     if (i < f.n) table[f.dst + i] = f.src < 0 ? f.value : table[f.src + i];
 }
 
-constexpr int MOVE_BYTES = 4 * 16 * 256;        // of one block: four pieces a thread in flight
+constexpr int MOVE_PIECES = 4 * 256;            // at most, of one block: four pieces of 16 bytes a thread in flight
 
 template <class ARGS> __global__ __launch_bounds__(256) void k_cache_move(ARGS list, CacheShape c)
 {
     const CacheMove m = cache_desc<CacheMove>(list, (size_t)blockIdx.x * sizeof(CacheMove));
     if (m.entry >= 0 && blockIdx.y == 0 && threadIdx.x == 0) c.table[m.entry] = m.dst;
     if (m.src < 0) return;
-    const uint4 *src = (const uint4 *)(c.pool + (size_t)m.src * c.page_bytes);
-    uint4 *dst = (uint4 *)(c.pool + (size_t)m.dst * c.page_bytes);
-    const int n = (int)(c.page_bytes / 16), at = blockIdx.y * (MOVE_BYTES / 16) + threadIdx.x;
-    uint4 v[4];
+    const u32x4 *src = (const u32x4 *)(as_global(c.pool) + (size_t)m.src * c.page_bytes);
+    u32x4 *dst = (u32x4 *)(as_global(c.pool) + (size_t)m.dst * c.page_bytes);
+    const int all = (int)(c.page_bytes / 16), each = (all + gridDim.y - 1) / gridDim.y;         // a page's blocks share it evenly
+    const int at = blockIdx.y * each + threadIdx.x, end = min(all, (int)(blockIdx.y + 1) * each);
+    u32x4 v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (at + 256 * j < n) v[j] = src[at + 256 * j];
+        if (at + 256 * j < end) v[j] = __builtin_nontemporal_load(src + at + 256 * j);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (at + 256 * j < n) dst[at + 256 * j] = v[j];
+        if (at + 256 * j < end) __builtin_nontemporal_store(v[j], dst + at + 256 * j);
 }
 
 }  // namespace
@@ -213,7 +217,7 @@ hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStr
 {
     if (moves.n == 0) return hipSuccess;
     return cache_launch(moves, [&](auto args) {
-        hipLaunchKernelGGL((k_cache_move<decltype(args)>), dim3(moves.n, (unsigned)((c.page_bytes + MOVE_BYTES - 1) / MOVE_BYTES)), dim3(256), 0, s, args, c);
+        hipLaunchKernelGGL((k_cache_move<decltype(args)>), dim3(moves.n, (unsigned)((c.page_bytes / 16 + MOVE_PIECES - 1) / MOVE_PIECES)), dim3(256), 0, s, args, c);
     });
 }
 
