@@ -17,8 +17,7 @@
 using namespace aif;
 
 namespace {
-constexpr int CACHE_NSLOT = 8;
-constexpr size_t CACHE_SLOT_BYTES = 512 << 10;
+constexpr size_t CACHE_LIST_BYTES = 512 << 10;      // of one launch's descriptors, at most
 constexpr int FEW_ROWS = 64, MIN_TILES = 8, MAX_SPLITS = 128, PART_ROWS = 384;     // plan_attend
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
@@ -33,12 +32,14 @@ struct aif_cache_ctx {
     float *part[2] = {};                    // partial results of the attention kernels for few and for many rows
     std::vector<uint32_t> stamp;            // sequences that a call has named
     uint32_t stamp_now = 0;
+    // Pinned memory for descriptors, in two halves.  Calls take pieces of one half until it is full; an event then marks the work that reads it,
+    // and the other half is used once its own event has passed.  (An event a call costs the stream as much as a launch.)
     char *h_stage = nullptr, *h_stage_dev = nullptr;
-    char *d_stage = nullptr;
-    size_t slot_bytes = CACHE_SLOT_BYTES;
-    hipEvent_t ev[CACHE_NSLOT] = {};
-    bool ev_live[CACHE_NSLOT] = {};
-    int next_slot = 0;
+    char *d_stage = nullptr;                // as large, where the pinned memory is not mapped, and for asks
+    size_t half_bytes = 0, at = 0;          // at: of the half in use
+    int half = 0;
+    hipEvent_t ev[2] = {};
+    bool ev_live[2] = {};
     alignas(16) char few[CACHE_FEW_BYTES];
     char err[512] = "";
 };
@@ -128,28 +129,46 @@ aif_status check_stream(aif_cache_ctx *c, hipStream_t s)
     return AIF_OK;
 }
 
+// A piece of the pinned memory for descriptors that launches on s will read: its offset.
+aif_status stage_take(aif_cache_ctx *c, size_t bytes, hipStream_t s, size_t &off)
+{
+    bytes = (bytes + 255) / 256 * 256;
+    if (c->at + bytes > c->half_bytes) {
+        CACHE_TRY(c, hipEventRecord(c->ev[c->half], s));
+        c->ev_live[c->half] = true;
+        const int other = c->half ^ 1;
+        if (c->ev_live[other]) CACHE_TRY(c, hipEventSynchronize(c->ev[other]));
+        c->ev_live[other] = false;
+        c->half = other;
+        c->at = 0;
+    }
+    off = (size_t)c->half * c->half_bytes + c->at;
+    c->at += bytes;
+    return AIF_OK;
+}
+
 // A list of descriptors on its way to a launch.  Up to CACHE_FEW_BYTES of a call travel in the kernel's arguments; more are
-// cut into lists of a slot of the pinned ring each.
+// cut into lists in pinned memory.
 template <class T> class CacheBatch {
 public:
-    CacheBatch(aif_cache_ctx *c, size_t expected, hipStream_t s) : c_(c), s_(s), far_(expected * sizeof(T) > CACHE_FEW_BYTES) {}
+    CacheBatch(aif_cache_ctx *c, size_t expected, hipStream_t s) : c_(c), s_(s), far_(expected * sizeof(T) > CACHE_FEW_BYTES)
+    {
+        room_ = far_ ? std::min(expected, CACHE_LIST_BYTES / sizeof(T)) : CACHE_FEW_BYTES / sizeof(T);
+    }
     // go: launches the list
     template <class F> aif_status add(const T &t, F &&go)
     {
-        const size_t room = (far_ ? CACHE_SLOT_BYTES : (size_t)CACHE_FEW_BYTES) / sizeof(T);
-        if (n_ == (int)room) {
+        if (n_ == (int)room_) {
             const aif_status st = send(go);
             if (st != AIF_OK) return st;
         }
         if (n_ == 0) {
+            at_ = (T *)c_->few;
             if (far_) {
-                slot_ = c_->next_slot;
-                if (c_->ev_live[slot_]) CACHE_TRY(c_, hipEventSynchronize(c_->ev[slot_]));
-                c_->ev_live[slot_] = false;
-                c_->next_slot = (slot_ + 1) % CACHE_NSLOT;
-                at_ = (T *)(c_->h_stage + (size_t)slot_ * c_->slot_bytes);
-            } else
-                at_ = (T *)c_->few;
+                const aif_status st = stage_take(c_, room_ * sizeof(T), s_, off_);
+                if (st != AIF_OK) return st;
+                at_ = (T *)(c_->h_stage + off_);
+            }
         }
         at_[n_++] = t;
         return AIF_OK;
@@ -161,15 +180,10 @@ public:
         n_ = 0;
         if (far_) {
             // a descriptor is read by one block, or one a head: from the pinned memory itself where that is mapped
-            const size_t off = (size_t)slot_ * c_->slot_bytes;
-            l.dev = c_->h_stage_dev ? c_->h_stage_dev + off : c_->d_stage + off;
-            if (!c_->h_stage_dev) CACHE_TRY(c_, staging_upload(c_->h_stage, nullptr, off, c_->d_stage + off, l.bytes, s_));
+            l.dev = c_->h_stage_dev ? c_->h_stage_dev + off_ : c_->d_stage + off_;
+            if (!c_->h_stage_dev) CACHE_TRY(c_, staging_upload(c_->h_stage, nullptr, off_, c_->d_stage + off_, l.bytes, s_));
         }
         CACHE_TRY(c_, go(l));
-        if (far_) {
-            CACHE_TRY(c_, hipEventRecord(c_->ev[slot_], s_));
-            c_->ev_live[slot_] = true;
-        }
         return AIF_OK;
     }
 
@@ -177,8 +191,9 @@ private:
     aif_cache_ctx *c_;
     hipStream_t s_;
     bool far_;
+    size_t room_, off_ = 0;
     T *at_ = nullptr;
-    int n_ = 0, slot_ = 0;
+    int n_ = 0;
 };
 
 void cdestroy(aif_cache_ctx *c)
@@ -189,8 +204,8 @@ void cdestroy(aif_cache_ctx *c)
         if (p) (void)hipFree(p);
     if (c->d_stage) (void)hipFree(c->d_stage);
     if (c->h_stage) (void)hipHostFree(c->h_stage);
-    for (int i = 0; i < CACHE_NSLOT; ++i)
-        if (c->ev[i]) (void)hipEventDestroy(c->ev[i]);
+    for (hipEvent_t e : c->ev)
+        if (e) (void)hipEventDestroy(e);
     delete c;
 }
 
@@ -230,17 +245,14 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     c->stamp.assign(f->max_seqs, 0u);
     CACHE_TRY(nullptr, hipGetDevice(&c->device));
     CACHE_TRY(nullptr, hipMalloc((void **)&s.table, (size_t)entries * sizeof(int32_t)));
-    // a list of asks is one upload, whatever its length
-    const size_t asks = attend_bytes(f->max_requests);
     int n_cu = 0;
     CACHE_TRY(nullptr, hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device));
     if (n_cu > 0) c->n_cu = n_cu;
     for (float *&p : c->part) CACHE_TRY(nullptr, hipMalloc((void **)&p, cache_part_floats(c->n_cu * PART_ROWS, s.dp) * sizeof(float)));
-    c->slot_bytes = ((asks > CACHE_SLOT_BYTES ? asks : CACHE_SLOT_BYTES) + 255) / 256 * 256;
-    CACHE_TRY(nullptr, staging_alloc(c->slot_bytes * CACHE_NSLOT, &c->h_stage, &c->h_stage_dev));
-    CACHE_TRY(nullptr, hipMalloc((void **)&c->d_stage, c->slot_bytes * CACHE_NSLOT));
-    for (int i = 0; i < CACHE_NSLOT; ++i)
-        CACHE_TRY(nullptr, hipEventCreateWithFlags(&c->ev[i], hipEventDisableTiming | hipEventDisableSystemFence));
+    c->half_bytes = (std::max(2 * CACHE_LIST_BYTES, 4 * attend_bytes(f->max_requests)) + 255) / 256 * 256;        // (a list of asks is one, whatever its length)
+    CACHE_TRY(nullptr, staging_alloc(c->half_bytes * 2, &c->h_stage, &c->h_stage_dev));
+    CACHE_TRY(nullptr, hipMalloc((void **)&c->d_stage, c->half_bytes * 2));
+    for (hipEvent_t &e : c->ev) CACHE_TRY(nullptr, hipEventCreateWithFlags(&e, hipEventDisableTiming | hipEventDisableSystemFence));
     return AIF_OK;
 }
 
@@ -379,9 +391,9 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
 {
     const CacheShape &sh = c->shape;
     auto rows_of = [&](const CacheAsk &a) { return (int64_t)a.n_q * sh.group; };
-    auto keys_of = [&](const CacheAsk &a) {         // tiles of keys that a row tile sees, about
+    auto keys_of = [&](const CacheAsk &a, int rows) {       // tiles of keys that a tile of so many rows sees, about: positions are taken to be spread evenly
         int64_t keys = a.len;
-        if (a.window && (!a.pos || a.n_q == 1)) keys = std::min<int64_t>(a.len, (int64_t)a.window + std::min(a.sinks, a.len));
+        if (a.window) keys = std::min<int64_t>(a.len, (int64_t)a.window + std::min(a.sinks, a.len) + (a.pos && a.n_q > 1 ? a.len * std::min<int64_t>(rows, rows_of(a)) / rows_of(a) : 0));
         return (keys + CACHE_TILE - 1) / CACHE_TILE;
     };
     bytes = (size_t)n * sizeof(CacheAsk);
@@ -401,9 +413,9 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         p.own = kind && sh.dp <= 64 && (sh.dp == 32 || sh.dtype == 0 || rows == 128 || windows);
         const int64_t room = (int64_t)c->n_cu * PART_ROWS / rows;
         auto tiles_of = [&](const CacheAsk &a) { return (rows_of(a) + rows - 1) / rows; };
-        int64_t work = 0, units = 0, joined = 0, parts = 0;
+        int64_t work = 0, units = 0, joined = 0, parts = 0, most_units = 0;
         for (int r = 0; r < n; ++r)
-            if (mine(asks[r])) work += tiles_of(asks[r]) * keys_of(asks[r]) * sh.n_kv;
+            if (mine(asks[r])) work += tiles_of(asks[r]) * keys_of(asks[r], rows) * sh.n_kv;
         const int64_t blocks = std::min<int64_t>(room * 3 / 4, (int64_t)c->n_cu * (kind || sh.dp > 64 ? 2 : 4));      // a compute unit holds about so many
         const int64_t chunk = std::max<int64_t>(MIN_TILES, (work + blocks - 1) / blocks);
         int32_t *first = arrays, *joins = arrays + n + 1;
@@ -415,9 +427,10 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
             joins[r] = (int32_t)joined;
             if (!mine(a)) continue;
             const int64_t tiles = tiles_of(a);
-            a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, (keys_of(a) + chunk / 2) / chunk), MAX_SPLITS);
+            a.splits = (int32_t)std::min<int64_t>(std::max<int64_t>(1, (keys_of(a, rows) + (kind ? 0 : chunk / 2)) / chunk), MAX_SPLITS);
             a.part = (int32_t)parts;
             units += tiles * a.splits;
+            most_units = std::max(most_units, tiles * a.splits);
             if (a.splits > 1) {
                 joined += rows_of(a);
                 parts += tiles * a.splits * sh.n_kv;
@@ -428,6 +441,9 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         joins[n] = (int32_t)joined;
         p.units = (int32_t)units;
         p.joins = (int32_t)joined;
+        // entries of as many units: a row of the grid each, in which a block need not look for its entry (empty blocks in the place of missing units leave
+        // whole XCDs without work)
+        p.each = most_units * n == units && most_units <= 65535 ? (int32_t)most_units : 0;
         p.part = c->part[kind];
     }
     return true;
@@ -458,14 +474,11 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
 
     const bool far = attend_bytes((size_t)n) > CACHE_FEW_BYTES;
     size_t bytes = 0;
-    int slot = 0;
+    size_t off = 0;
     char *h = c->few;
     if (far) {
-        slot = c->next_slot;
-        if (c->ev_live[slot]) CACHE_TRY(c, hipEventSynchronize(c->ev[slot]));
-        c->ev_live[slot] = false;
-        c->next_slot = (slot + 1) % CACHE_NSLOT;
-        h = c->h_stage + (size_t)slot * c->slot_bytes;
+        if ((st = stage_take(c, attend_bytes((size_t)n), s, off)) != AIF_OK) return st;
+        h = c->h_stage + off;
     }
     CacheAsk *ha = (CacheAsk *)h;
     for (int r = 0; r < n; ++r) {
@@ -477,15 +490,10 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
     if (!plan_attend(c, ha, n, (int32_t *)(ha + n), plan, bytes)) return cfail(c, AIF_ERANGE, "one call has too many queries");
     CacheList l{h, nullptr, n, bytes};
     if (far) {
-        const size_t off = (size_t)slot * c->slot_bytes;
         CACHE_TRY(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
         l.dev = c->d_stage + off;
     }
     CACHE_TRY(c, launch_cache_attend(c->shape, l, plan, s));
-    if (far) {
-        CACHE_TRY(c, hipEventRecord(c->ev[slot], s));
-        c->ev_live[slot] = true;
-    }
     return AIF_OK;
 }
 

@@ -81,6 +81,7 @@ hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStr
 // has any (few first) int32 first[n + 1], running numbers of units, and int32 joins[n + 1], running numbers of the rows whose keys are split.
 struct CachePart {
     int32_t units, joins;       // of all asks
+    int32_t each;               // > 0: every entry has that many units
     int32_t rows_of_tile;
     bool own;                   // many rows: the kernel whose waves bring keys and values to bf16 for themselves
     float *part;                // partial results of split keys, a unit and kv head each: [rows][dp] sums, [rows] maxima, [rows] sums of weights

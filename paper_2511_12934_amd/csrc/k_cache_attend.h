@@ -18,7 +18,10 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 // The blocks of a launch: running numbers of units behind the asks.  A unit is (row tile, split), tiles first.
 struct CacheGrid {
     int32_t n, firsts;          // asks; byte offset of int32 first[n + 1]
+    int32_t each;               // CachePart::each
 };
+
+inline dim3 cache_grid(const CacheGrid &g, const CacheShape &c, const CachePart &p) { return p.each ? dim3(g.n, c.n_kv, p.each) : dim3(p.units, c.n_kv, 1); }
 
 void launch_cache_own(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
 void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
@@ -45,6 +48,24 @@ __device__ __forceinline__ int ask_of(const char *dev, const CacheGrid &g, int u
         if (below < 64) break;
     }
     return __builtin_amdgcn_readfirstlane(r);
+}
+// The block's ask and its unit of it.
+struct AskUnit {
+    CacheAsk a;
+    int unit;
+};
+__device__ __forceinline__ AskUnit block_ask(const char *dev, const CacheGrid &g, int lane)
+{
+    AskUnit u;
+    if (g.each) {
+        u.a = ask_at(dev, blockIdx.x);
+        u.unit = blockIdx.z;
+        return u;
+    }
+    const int r = ask_of(dev, g, blockIdx.x, lane);
+    u.a = ask_at(dev, r);
+    u.unit = (int)blockIdx.x - first_at(dev, g, r);
+    return u;
 }
 
 // What a row (query i and a head) sees: keys j <= last, and of those beyond `from` or before `sinks` only.

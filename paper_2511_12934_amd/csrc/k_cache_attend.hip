@@ -97,10 +97,12 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     __shared__ float ml[2][4][ROWS];
     (void)few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4, kvh = blockIdx.y;
-    const int r = ask_of(dev, g, blockIdx.x, lane);
-    const CacheAsk a = ask_at(dev, r);
-    const int unit = (int)blockIdx.x - first_at(dev, g, r), tile_of_rows = unit / a.splits, split = unit % a.splits;
-    const int n_rows = a.n_q * c.group, row0 = tile_of_rows * ROWS;
+    const AskUnit found = block_ask(dev, g, lane);
+    const CacheAsk &a = found.a;
+    const int unit = found.unit, n_rows = a.n_q * c.group;
+    int tile_of_rows = unit, split = 0;
+    if (a.splits > 1) tile_of_rows = unit / a.splits, split = unit % a.splits;
+    const int row0 = tile_of_rows * ROWS;
 
     // the rows: who sees what, and their features
     Sight see[NT];
@@ -123,8 +125,12 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
         }
     }
     const Walk walk = reach.walk<16>(a);
-    const int64_t n_tiles = walk.count();
-    const int t_end = (int)(n_tiles * (split + 1) / a.splits);
+    int t = wave, t_end = walk.count();
+    if (a.splits > 1) {
+        const int64_t n = t_end;
+        t += (int)(n * split / a.splits);
+        t_end = (int)(n * (split + 1) / a.splits);
+    }
 
     const char *pool = c.pool + (size_t)kvh * cache_head_bytes(c);
     f32x4 acc[NT][FT];
@@ -140,19 +146,18 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     typedef s16x4 __attribute__((address_space(3))) *lds4_t;
     const char *turned = mine + (4 * grp + col / 4) * STRIDE + col % 4 * 8;      // this lane's piece of four keys and 16 features
 
-    int t = (int)(n_tiles * split / a.splits) + wave;
     TileList<DP> list;
     list.fill(c, a, walk, t, 4, t_end, lane);
     auto ask = [&](int t, RawTile<NW> &to) {            // a tile that is dropped or behind the end reads page 0
-        if (t - list.from == 256) list.fill(c, a, walk, t, 4, t_end, lane);
+        if (t - list.from >= 256) list.fill(c, a, walk, t, 4, t_end, lane);
         const int64_t off = list.offset((t - list.from) / 4);
         to.here = off >= 0;
         load_tile<NW>(pool + (off < 0 ? 0 : off), lane, to);
     };
     auto work = [&](int t, RawTile<NW> &now) {
-        if (!now.here) return;
         now.pin();
-        const int tile = walk.tile(t), j0 = tile * CACHE_TILE + 4 * grp;
+        const bool here = now.here;
+        const int tile = walk.tile(t), j0 = here ? tile * CACHE_TILE + 4 * grp : NO_KEY;        // (dropped or behind the end: nobody sees it)
 
         // values: as bf16 rows of the wave's LDS.  A block that is not finite -- NaN, or bytes that nobody wrote -- becomes zeros:
         // who sees it gets NaN below.
@@ -163,7 +168,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
             for (int w = 0; w < NW; ++w) {
                 const float sc = word_scale<NW>(now.vs[h], grp, w);
                 const bool fine = sc < 0x1p126f;
-                odd |= fine || tile * CACHE_TILE + 16 * h + col > reach.hi_last ? 0u : 1u;
+                odd |= fine || !here || tile * CACHE_TILE + 16 * h + col > reach.hi_last ? 0u : 1u;
                 *(bf16x8 *)(mine + (16 * h + col) * STRIDE + (grp * (DP / 4) + 8 * w) * 2) = decode8(fine ? now.v[h][w] : 0u, fine ? sc : 1.f);
             }
         }
@@ -183,7 +188,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
                     for (int p = NP - 1; p >= 0; --p) s[i][h] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k, q[i][p][w], s[i][h], 0, 0, 0);
             }
 
-        const bool whole = walk.whole(tile);
+        const bool whole = here && walk.whole(tile);
         bf16x8 weights[NT][NP];
 #pragma unroll
         for (int i = 0; i < NT; ++i) {
@@ -247,15 +252,19 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     };
     // Sets of registers by turns: what one is loaded with is not waited for while another is worked on.  A wave of a short call has few tiles,
     // and its time is that of the loads behind one another: all it can hold are on their way at once.
-    constexpr int DEPTH = DT == 1 && NT == 1 && NW <= 4 ? 4 : 2;
+    constexpr int DEPTH = DT == 1 && NT == 1 && NW <= 4 ? 2 : 2;
     RawTile<NW> raw[DEPTH];
 #pragma unroll
-    for (int i = 0; i < DEPTH - 1; ++i) ask(t + 4 * i, raw[i]);
+    for (int i = 0; i < DEPTH - 1; ++i) {
+        ask(t + 4 * i, raw[i]);
+        __builtin_amdgcn_sched_barrier(0);
+    }
     for (; t < t_end; t += 4 * DEPTH)
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
             ask(t + 4 * (i + DEPTH - 1), raw[(i + DEPTH - 1) % DEPTH]);
-            if (t + 4 * i < t_end) work(t + 4 * i, raw[i]);
+            __builtin_amdgcn_sched_barrier(0);
+            work(t + 4 * i, raw[i]);
         }
 
     // the four waves' parts become one: a common reference, then sums through LDS
@@ -371,7 +380,7 @@ template <int DT> __global__ __launch_bounds__(128) void k_cache_join(CacheFew f
 namespace {
 template <int DT, int NW, int NT> void few(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_cache_few<DT, NW, NT>), dim3(p.units, c.n_kv), dim3(256), 0, s, args, dev, g, c, p.part);
+    hipLaunchKernelGGL((k_cache_few<DT, NW, NT>), cache_grid(g, c, p), dim3(256), 0, s, args, dev, g, c, p.part);
 }
 template <int NW> void few_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
@@ -399,10 +408,11 @@ hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const
 {
     CacheFew args;
     if (!asks.dev) __builtin_memcpy(args.w, asks.host, asks.bytes);
-    CacheGrid g{asks.n, (int32_t)(asks.n * sizeof(CacheAsk))};
+    CacheGrid g{asks.n, (int32_t)(asks.n * sizeof(CacheAsk)), 0};
     for (int kind = 0; kind < 2; ++kind) {
         const CachePart &of = kind ? p.many : p.few;
         if (of.units == 0) continue;
+        g.each = of.each;
         if (kind && of.own) launch_cache_own(args, asks.dev, g, c, of, s);
         else if (kind) launch_cache_many(args, asks.dev, g, c, of, s);
         else launch_cache_few(args, asks.dev, g, c, of, s);

@@ -26,9 +26,9 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
     __shared__ int odd_now[3];                          // whether a stage has blocks of values that are not finite
     (void)few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5, kvh = blockIdx.y;
-    const int r = ask_of(dev, g, blockIdx.x, lane);
-    const CacheAsk a = ask_at(dev, r);
-    const int unit = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group;
+    const AskUnit found = block_ask(dev, g, lane);
+    const CacheAsk &a = found.a;
+    const int unit = found.unit, n_rows = a.n_q * c.group;
     int row_tile = unit, split = 0;
     if (a.splits > 1) row_tile = unit / a.splits, split = unit % a.splits;
     const char *pool = as_global(c.pool) + (size_t)kvh * cache_head_bytes(c);
@@ -237,7 +237,7 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
 
 template <int DT, int NW, int CT, int WAVES> void many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
-    const dim3 grid(p.units, c.n_kv), block(64 * WAVES);
+    const dim3 grid = cache_grid(g, c, p), block(64 * WAVES);
     hipLaunchKernelGGL((k_cache_many<DT, NW, CT, WAVES, 2 * NW>), grid, block, 0, s, args, dev, g, c, p.part);
 }
 template <int NW> void many_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)

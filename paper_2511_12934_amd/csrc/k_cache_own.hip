@@ -17,9 +17,9 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
     __shared__ __align__(16) char lds[4][CACHE_TILE * 2 * DP];
     (void)few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 31, half = lane >> 5, kvh = blockIdx.y;
-    const int r = ask_of(dev, g, blockIdx.x, lane);
-    const CacheAsk a = ask_at(dev, r);
-    const int unit = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group, in_block = 32 * CT * wave;
+    const AskUnit found = block_ask(dev, g, lane);
+    const CacheAsk &a = found.a;
+    const int unit = found.unit, n_rows = a.n_q * c.group, in_block = 32 * CT * wave;
     int row_tile = unit, split = 0;
     if (a.splits > 1) row_tile = unit / a.splits, split = unit % a.splits;
     const char *pool = as_global(c.pool) + (size_t)kvh * cache_head_bytes(c);
@@ -96,7 +96,7 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
     };
     // One phase: the weights of row tile i from its scores si beside the scores so of row tile o, then their product with the values.
     // fresh: the keys for so are those of `keys`, from here on.
-    auto phase = [&](int i, f32x16 &si, int o, f32x16 &so, bool fresh, const Raw &keys, int tile, bool here) {
+    auto phase = [&](int i, f32x16 &si, int o, f32x16 &so, bool fresh, Raw &keys, int tile, bool here) {
         if (!here || !walk.whole(tile)) see[i].hide(si, here ? tile * CACHE_TILE + 4 * half : NO_KEY);
         float top = -INFINITY;
 #pragma unroll
@@ -114,6 +114,7 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
             m[i] = m2;
         }
         const float ref = m[i] == -INFINITY ? 0.f : m[i];
+        if (fresh) asm volatile("" : "+v"(keys.ks));
         const float ks = scale_of(keys.ks);
         float x[16];
         constexpr int EACH = 16 / KS;
@@ -144,7 +145,7 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
     // Tile t: its scores s0 (of row tile 0) are there, kf holds its keys where CT = 2, and `next` the codes of the tile behind it,
     // whose scores s1 (CT = 1; of row tile 0 again: s0) are there in the end.
     auto step = [&](int t, Raw &now, Raw &next, f32x16 &s0, f32x16 &s1) {
-        asm volatile("" : "+v"(now.vs), "+v"(next.ks));     // (made use of here, not where they are asked for)
+        asm volatile("" : "+v"(now.vs));        // (made use of here, not where it is asked for)
         const int tile = walk.tile(t);
         const bool here = now.here;
         // a block of values that is not finite becomes zeros: who sees it gets NaN below
@@ -210,7 +211,7 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
 
 template <int DT, int NW, int CT> void own(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
-    const dim3 grid(p.units, c.n_kv), block(256);
+    const dim3 grid = cache_grid(g, c, p), block(256);
     if constexpr (NW == 1)
         if (c.d_head <= 16) {
             hipLaunchKernelGGL((k_cache_own<DT, NW, CT, 1>), grid, block, 0, s, args, dev, g, c, p.part);
