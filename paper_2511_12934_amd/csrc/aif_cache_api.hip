@@ -18,7 +18,7 @@ using namespace aif;
 
 namespace {
 constexpr size_t CACHE_LIST_BYTES = 512 << 10;      // of one launch's descriptors, at most
-constexpr int FEW_ROWS = 64, MIN_TILES = 8, MAX_SPLITS = 128, PART_ROWS = 384;     // plan_attend
+constexpr int FEW_ROWS = 64, MIN_TILES = 8, FEW_TILES = 3, MAX_SPLITS = 128, PART_ROWS = 384;     // plan_attend
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
 }  // namespace
@@ -384,7 +384,9 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
 // How a call's work is cut.  Entries of up to FEW_ROWS rows (queries times heads of a kv head) go to the kernel whose row tiles are 16 or 32
 // (fp32: 16, a query's three pieces take the registers), the others to the one whose tiles are 128 or, bf16 heads of up to 128 and
 // enough of them, 256.  Where the (row tile, kv head) pairs are fewer than the device holds blocks, their keys are shared
-// out as well, in splits of at least MIN_TILES tiles of 32 keys, so that a split outlasts its start.  Partial results have room for
+// out as well, in splits of at least MIN_TILES tiles of 32 keys, so that a split outlasts its start (many rows, but fewer than a quarter of the
+// device's: FEW_TILES, since a wave there works on its tiles one after the other and the join is short: three users of 183 rows 18 -> 14 us;
+// 16 users of 2,000 rows with as small splits 13 -> 30).  Partial results have room for
 // PART_ROWS rows a compute unit and kernel: keys / chunk is rounded, by a third up at most where that makes two or more, and
 // tiles * keys / chunk <= work / chunk <= 3 / 4 of the room.
 static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays, CachePlan &plan, size_t &bytes)
@@ -413,11 +415,11 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         p.own = kind && sh.dp <= 64 && (sh.dp == 32 || sh.dtype == 0 || rows == 128 || windows);
         const int64_t room = (int64_t)c->n_cu * PART_ROWS / rows;
         auto tiles_of = [&](const CacheAsk &a) { return (rows_of(a) + rows - 1) / rows; };
-        int64_t work = 0, units = 0, joined = 0, parts = 0, most_units = 0;
+        int64_t work = 0, all = 0, units = 0, joined = 0, parts = 0, most_units = 0;
         for (int r = 0; r < n; ++r)
-            if (mine(asks[r])) work += tiles_of(asks[r]) * keys_of(asks[r], rows) * sh.n_kv;
+            if (mine(asks[r])) work += tiles_of(asks[r]) * keys_of(asks[r], rows) * sh.n_kv, all += tiles_of(asks[r]) * sh.n_kv;
         const int64_t blocks = std::min<int64_t>(room * 3 / 4, (int64_t)c->n_cu * (kind || sh.dp > 64 ? 2 : 4));      // a compute unit holds about so many
-        const int64_t chunk = std::max<int64_t>(MIN_TILES, (work + blocks - 1) / blocks);
+        const int64_t chunk = std::max<int64_t>(kind && 4 * all < c->n_cu ? FEW_TILES : MIN_TILES, (work + blocks - 1) / blocks);
         int32_t *first = arrays, *joins = arrays + n + 1;
         arrays += 2 * (n + 1);
         bytes += 2 * ((size_t)n + 1) * sizeof(int32_t);

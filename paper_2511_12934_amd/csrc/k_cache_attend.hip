@@ -104,25 +104,15 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     if (a.splits > 1) tile_of_rows = unit / a.splits, split = unit % a.splits;
     const int row0 = tile_of_rows * ROWS;
 
-    // the rows: who sees what, and their features
+    RowOf rows[NT];
     Sight see[NT];
-    bf16x8 q[NT][NP][NW];
     Reach reach;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int row = row0 + 16 * t + col;
-        const bool is_row = row < n_rows;
-        const RowOf o = row_of(c, kvh, is_row ? row : 0);
-        see[t] = sight_of(a, o.i, is_row);
-        reach.add(see[t], is_row);
-        const char *qr = a.q + (size_t)o.i * a.q_stride + (size_t)o.head * c.d_head * (DT == 0 ? 4 : 2);
-#pragma unroll
-        for (int w = 0; w < NW; ++w) {
-            bf16x8 p[NP];
-            query8<DT, NP>(qr, grp * (DP / 4) + 8 * w, c.d_head, is_row, p);
-#pragma unroll
-            for (int i = 0; i < NP; ++i) q[t][i][w] = p[i];
-        }
+    for (int i = 0; i < NT; ++i) {
+        const int row = row0 + 16 * i + col;
+        rows[i] = row_of(c, kvh, row < n_rows ? row : 0);
+        see[i] = sight_of(a, rows[i].i, row < n_rows);
+        reach.add(see[i], row < n_rows);
     }
     const Walk walk = reach.walk<16>(a);
     int t = wave, t_end = walk.count();
@@ -132,7 +122,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
         t_end = (int)(n * (split + 1) / a.splits);
     }
 
-    const char *pool = c.pool + (size_t)kvh * cache_head_bytes(c);
+    const char *pool = as_global(c.pool) + (size_t)kvh * cache_head_bytes(c);
     f32x4 acc[NT][FT];
     float m[NT], l[NT];
 #pragma unroll
@@ -154,6 +144,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
         to.here = off >= 0;
         load_tile<NW>(pool + (off < 0 ? 0 : off), lane, to);
     };
+    bf16x8 q[NT][NP][NW];
     auto work = [&](int t, RawTile<NW> &now) {
         now.pin();
         const bool here = now.here;
@@ -258,6 +249,17 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     for (int i = 0; i < DEPTH - 1; ++i) {
         ask(t + 4 * i, raw[i]);
         __builtin_amdgcn_sched_barrier(0);
+    }
+#pragma unroll
+    for (int i = 0; i < NT; ++i) {              // (the queries come while the first tiles do)
+        const char *qr = a.q + (size_t)rows[i].i * a.q_stride + (size_t)rows[i].head * c.d_head * (DT == 0 ? 4 : 2);
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            bf16x8 p[NP];
+            query8<DT, NP>(qr, grp * (DP / 4) + 8 * w, c.d_head, row0 + 16 * i + col < n_rows, p);
+#pragma unroll
+            for (int j = 0; j < NP; ++j) q[i][j][w] = p[j];
+        }
     }
     for (; t < t_end; t += 4 * DEPTH)
 #pragma unroll

@@ -36,11 +36,10 @@ template <int DT, int NW, int CT, int WAVES, int KS> __global__ __launch_bounds_
     typedef s16x4 __attribute__((address_space(3))) *lds4_t;
     const int row0 = row_tile * ROWS;
 
-
     Reach reach;
     if (a.pos) {
         for (int i = lane; i < ROWS; i += 64)
-            if (row0 + i < n_rows) reach.add(sight_of(a, (row0 + i) / c.group, true), true);
+            if (row0 + i < n_rows) reach.add(sight_of(a, row_of(c, 0, row0 + i).i, true), true);
     } else
         reach.add(sight_of(a, 0, true), true);
     const Walk walk = reach.walk<64>(a);

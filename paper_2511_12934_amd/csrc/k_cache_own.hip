@@ -29,25 +29,15 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
     const int row0 = row_tile * ROWS + in_block;
     if (row0 >= n_rows) return;                 // no wave waits for another
 
-
+    RowOf rows[CT];
     Sight see[CT];
-    bf16x8 q[CT][NP][KS];
     Reach reach;
 #pragma unroll
-    for (int t = 0; t < CT; ++t) {
-        const int row = row0 + 32 * t + col;
-        const bool is_row = row < n_rows;
-        const RowOf o = row_of(c, kvh, is_row ? row : row0);
-        see[t] = sight_of(a, o.i, is_row);
-        reach.add(see[t], is_row);
-        const char *qr = a.q + (size_t)o.i * a.q_stride + (size_t)o.head * c.d_head * (DT == 0 ? 4 : 2);
-#pragma unroll
-        for (int k = 0; k < KS; ++k) {
-            bf16x8 p[NP];
-            query8<DT, NP>(qr, half * (8 * KS) + 8 * k, c.d_head, is_row, p);
-#pragma unroll
-            for (int i = 0; i < NP; ++i) q[t][i][k] = p[i];
-        }
+    for (int i = 0; i < CT; ++i) {
+        const int row = row0 + 32 * i + col;
+        rows[i] = row_of(c, kvh, row < n_rows ? row : row0);
+        see[i] = sight_of(a, rows[i].i, row < n_rows);
+        reach.add(see[i], row < n_rows);
     }
     const Walk walk = reach.walk<32>(a);
     int t = 0, t_end = walk.count();
@@ -85,7 +75,7 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
         raw.here = off >= 0;
     };
 
-    bf16x8 kf[KS], vf[2][NW];
+    bf16x8 q[CT][NP][KS], kf[KS], vf[2][NW];
     // The first product of row tile o of a tile whose keys kf holds, or, `fresh`, has yet to hold: step k of it.
     auto scores = [&](int o, int k, f32x16 &so) {
         if (k == 0)
@@ -191,6 +181,17 @@ template <int DT, int NW, int CT, int KS> __global__ __launch_bounds__(256, 2) v
     f32x16 s0, s1;
     ask(t, raw0);
     ask(t + 1, raw1);
+#pragma unroll
+    for (int i = 0; i < CT; ++i) {              // (the queries come while the first tiles do)
+        const char *qr = a.q + (size_t)rows[i].i * a.q_stride + (size_t)rows[i].head * c.d_head * (DT == 0 ? 4 : 2);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            bf16x8 p[NP];
+            query8<DT, NP>(qr, half * (8 * KS) + 8 * k, c.d_head, row0 + 32 * i + col < n_rows, p);
+#pragma unroll
+            for (int j = 0; j < NP; ++j) q[i][j][k] = p[j];
+        }
+    }
     asm volatile("" : "+v"(raw0.ks));
 #pragma unroll
     for (int k = 0; k < KS; ++k) {
