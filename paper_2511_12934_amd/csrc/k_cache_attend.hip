@@ -10,8 +10,7 @@
 // the 16x16x32 products: S^T = K Q^T (a lane's codes of a key are the k-slots; which features stand in which slot is free, so a
 // lane takes dp / 4 neighbouring ones), whose result leaves a lane with eight keys of ONE row: the weights are the second
 // product's operand where they are, O^T = V^T P^T.  V has to be turned, features to rows: bf16 rows of 32 keys in the wave's own LDS,
-// read back by ds_read_b64_tr_b16 (four keys of one feature a lane); rows are 32 bytes longer than their features, so that
-// eight rows' pieces lie in different banks.  No barrier in the loop; the four waves of a block take the tiles in turn, each
+// read back by ds_read_b64_tr_b16 (four keys of one feature a lane; v_place keeps the lanes to different banks).  No barrier in the loop; the four waves of a block take the tiles in turn, each
 // with the next tile's codes already asked for, and join through LDS.
 #include "k_cache_attend.h"
 
@@ -88,13 +87,25 @@ template <int NW> __device__ __forceinline__ float word_scale(const uint32_t (&b
     return scale_of(b);
 }
 
+// Four features of a row from their sums o, the row's reference m and its sum of weights; the row's logarithm with the first of them.
+template <int DT> __device__ __forceinline__ void store_row(const CacheAsk &a, const CacheShape &c, int kvh, int row, int f, const f32x4 &o, float m, float sum)
+{
+    const RowOf at = row_of(c, kvh, row);
+    if (f == 0 && a.lse) as_global(a.lse)[(size_t)at.i * c.n_heads + at.head] = sum == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(sum)) * LN2;
+    if (f >= c.d_head) return;
+    const f32x4 v = sum == 0.f ? f32x4{0.f, 0.f, 0.f, 0.f} : o * (1.f / sum);
+    char *out = as_global(a.out) + (size_t)at.i * a.out_stride + ((size_t)at.head * c.d_head + f) * (DT == 0 ? 4 : 2);
+    if constexpr (DT == 0) *(f32x4 *)out = v;
+    else *(bf16x4 *)out = __builtin_convertvector(v, bf16x4);
+}
+
 template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache_few(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
 {
     constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 16 * NT, FT = DP / 16;
-    constexpr int STRIDE = 2 * DP + 32, WAVE_BYTES = 32 * STRIDE;
-    static_assert(WAVE_BYTES >= 16 * DP * 4, "a wave's sums fit its room for values");
+    constexpr int WAVE_BYTES = 64 * DP + 256;       // 32 rows of values; in the end 16 rows of sums, four apart
+    static_assert(WAVE_BYTES == 16 * (DP + 4) * 4);
     __shared__ __align__(16) char lds[4 * WAVE_BYTES];
-    __shared__ float ml[2][4][ROWS];
+    __shared__ float ml[2][4][ROWS], total[2][ROWS];
     (void)few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4, kvh = blockIdx.y;
     const AskUnit found = block_ask(dev, g, lane);
@@ -134,7 +145,6 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     const float k2 = c.scale * LOG2E;
     char *mine = lds + wave * WAVE_BYTES;
     typedef s16x4 __attribute__((address_space(3))) *lds4_t;
-    const char *turned = mine + (4 * grp + col / 4) * STRIDE + col % 4 * 8;      // this lane's piece of four keys and 16 features
 
     TileList<DP> list;
     list.fill(c, a, walk, t, 4, t_end, lane);
@@ -160,7 +170,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
                 const float sc = word_scale<NW>(now.vs[h], grp, w);
                 const bool fine = sc < 0x1p126f;
                 odd |= fine || !here || tile * CACHE_TILE + 16 * h + col > reach.hi_last ? 0u : 1u;
-                *(bf16x8 *)(mine + (16 * h + col) * STRIDE + (grp * (DP / 4) + 8 * w) * 2) = decode8(fine ? now.v[h][w] : 0u, fine ? sc : 1.f);
+                *(bf16x8 *)(mine + v_place<DP>(16 * h + col, grp * NW + w)) = decode8(fine ? now.v[h][w] : 0u, fine ? sc : 1.f);
             }
         }
 
@@ -216,8 +226,8 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
                 s16x4 h[2];
                 bf16x8 all;
             } v;
-            v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turned + f * 32));
-            v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(turned + 16 * STRIDE + f * 32));
+            v.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(mine + v_turned<DP>(4 * grp, 16 * f, lane)));
+            v.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4_t)(mine + v_turned<DP>(16 + 4 * grp, 16 * f, lane)));
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -277,45 +287,44 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
         if (grp == 0) ml[0][wave][16 * i + col] = m[i], ml[1][wave][16 * i + col] = l[i];
     }
     __syncthreads();
-    const int esz = DT == 0 ? 4 : 2;
-    float *pt = part + ((size_t)a.part + (size_t)kvh * ((n_rows + ROWS - 1) / ROWS) * a.splits + unit) * cache_part_floats(ROWS, DP);    // (splits > 1)
+    const int rows_here = min(ROWS, n_rows - row0);
+    const size_t each = cache_part_floats(ROWS, DP);
+    const size_t first_part = (size_t)a.part + (size_t)(kvh * ((n_rows + ROWS - 1) / ROWS) + tile_of_rows) * a.splits;     // (splits > 1)
+    float *pt = as_global(part) + (first_part + split) * each;
+    if (threadIdx.x < ROWS) {
+        float mt = -INFINITY, sum = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mt = fmaxf(mt, ml[0][w][threadIdx.x]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float mw = ml[0][w][threadIdx.x];
+            sum += mw == -INFINITY ? ml[1][w][threadIdx.x] : ml[1][w][threadIdx.x] * __builtin_amdgcn_exp2f(mw - mt);    // (no maximum: 0, or NaN)
+        }
+        total[0][threadIdx.x] = mt, total[1][threadIdx.x] = sum;
+    }
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) top = fmaxf(top, ml[0][w][16 * i + col]);
+        if (16 * i >= rows_here) break;
+        const float top = total[0][16 * i + col];
         const float back = m[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[i] - top);
-        float *sums = (float *)mine;            // [16 rows][DP]
+        f32x4 *sums = (f32x4 *)mine;            // [16 rows][DP + 4]
         if (i) __syncthreads();
+        if (16 * i + col < rows_here) {
 #pragma unroll
-        for (int f = 0; f < FT; ++f)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) sums[col * DP + 16 * f + 4 * grp + e] = m[i] == -INFINITY ? acc[i][f][e] * 0.f : acc[i][f][e] * back;
+            for (int f = 0; f < FT; ++f) sums[(col * (DP + 4) + 16 * f + 4 * grp) / 4] = acc[i][f] * back;
+        }
         __syncthreads();
-        for (int x = threadIdx.x; x < 16 * DP; x += 256) {
-            const int cl = x / DP, f = x % DP, row = row0 + 16 * i + cl;
-            float mt = -INFINITY, sum = 0.f, o = 0.f;
+        for (int x = threadIdx.x; x < min(16, rows_here - 16 * i) * (DP / 4); x += 256) {
+            const int cl = x / (DP / 4), f = x % (DP / 4) * 4, row = row0 + 16 * i + cl;
+            f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) mt = fmaxf(mt, ml[0][w][16 * i + cl]);
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                o += ((const float *)(lds + w * WAVE_BYTES))[x];
-                const float mw = ml[0][w][16 * i + cl];
-                sum += mw == -INFINITY ? ml[1][w][16 * i + cl] : ml[1][w][16 * i + cl] * __builtin_amdgcn_exp2f(mw - mt);
-            }
+            for (int w = 0; w < 4; ++w) o += ((const f32x4 *)(lds + w * WAVE_BYTES))[(cl * (DP + 4) + f) / 4];
             if (a.splits > 1) {
-                pt[(16 * i + cl) * DP + f] = o;
-                if (f == 0) pt[ROWS * DP + 16 * i + cl] = mt, pt[ROWS * DP + ROWS + 16 * i + cl] = sum;
-            } else if (row < n_rows) {
-                const RowOf at_row = row_of(c, kvh, row);
-                const float v = sum == 0.f ? 0.f : o / sum;
-                if (f < c.d_head) {
-                    char *out = a.out + (size_t)at_row.i * a.out_stride + ((size_t)at_row.head * c.d_head + f) * esz;
-                    if (DT == 0) *(float *)out = v;
-                    else *(uint16_t *)out = f2bf(v);
-                }
-                if (f == 0 && a.lse) a.lse[(size_t)at_row.i * c.n_heads + at_row.head] = sum == 0.f ? -INFINITY : (mt + __builtin_amdgcn_logf(sum)) * LN2;
-            }
+                *(f32x4 *)(pt + (16 * i + cl) * DP + f) = o;
+                if (f == 0) pt[ROWS * DP + 16 * i + cl] = total[0][16 * i + cl], pt[ROWS * DP + ROWS + 16 * i + cl] = total[1][16 * i + cl];
+            } else
+                store_row<DT>(a, c, kvh, row, f, o, total[0][16 * i + cl], total[1][16 * i + cl]);
         }
     }
 }
