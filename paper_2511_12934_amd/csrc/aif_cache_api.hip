@@ -18,7 +18,7 @@ using namespace aif;
 
 namespace {
 constexpr size_t CACHE_LIST_BYTES = 512 << 10;      // of one launch's descriptors, at most
-constexpr int FEW_ROWS = 64, MIN_TILES = 8, FEW_TILES = 3, MAX_SPLITS = 128, PART_ROWS = 384;     // plan_attend
+constexpr int FEW_ROWS = 64, ROWS_OF_CU = 64, MIN_TILES = 4, MAX_SPLITS = 128, PART_ROWS = 384;     // plan_attend
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
 }  // namespace
@@ -381,14 +381,26 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
     return batch.send(go);
 }
 
-// How a call's work is cut.  Entries of up to FEW_ROWS rows (queries times heads of a kv head) go to the kernel whose row tiles are 16 or 32
-// (fp32: 16, a query's three pieces take the registers), the others to the one whose tiles are 128 or, bf16 heads of up to 128 and
-// enough of them, 256.  Where the (row tile, kv head) pairs are fewer than the device holds blocks, their keys are shared
-// out as well, in splits of at least MIN_TILES tiles of 32 keys, so that a split outlasts its start (many rows, but fewer than a quarter of the
-// device's: FEW_TILES, since a wave there works on its tiles one after the other and the join is short: three users of 183 rows 18 -> 14 us;
-// 16 users of 2,000 rows with as small splits 13 -> 30).  Partial results have room for
-// PART_ROWS rows a compute unit and kernel: keys / chunk is rounded, by a third up at most where that makes two or more, and
-// tiles * keys / chunk <= work / chunk <= 3 / 4 of the room.
+// How a call's work is cut: into tiles of rows (a row is a query and a head of a kv head's group) and, where that pays, splits of their keys.
+//
+// Which kernel.  The one for few rows has tiles of 16 or 32 (fp32: 16, a query's three pieces take the registers), whose keys four waves share; the others
+// have tiles of 128, or 256 for bf16 heads of up to 128 and two of them for each compute unit.  The small tiles are the quicker ones as long as
+// they do not queue: up to ROWS_OF_CU rows for a compute unit in the whole call (32 users x 256 queries, two heads of 128 over 800 keys 30 us, 36 in
+// tiles of 128; of 512 queries 57 and 37).  The price is one user's
+// long prompt: 16,000 queries over 10^5 keys, a head of 64: 820 us, 655.  In larger calls only entries of up to FEW_ROWS rows go there.
+//
+// Many rows: heads of up to 32 features, and fp32 up to 64, are the cheapest to bring to bf16 once a wave (8 x 10^4 rows of 8 heads of 16 over 2,000 keys 255
+// us, 276 once a block); up to 64 that also serves few row tiles, whose blocks wait for nobody, and rows that see each a window of its
+// own, of which a wave's span is less than a block's (replayed impressions 31 us, 48).
+//
+// Splits.  A second launch joins their results, so they must save more than that costs.  The estimate: a tile of rows takes `tile` us for each 32 keys, blocks of
+// one compute unit beside each other 0.8 times that each; a join takes 4 us, and its floats go and come at 1.8 TB/s.  (tile, from unsplit calls
+// over 800 and 3,000 keys: 32 bf16 rows of heads of 32, 64, 128, 256: 0.14, 0.18, 0.25, 0.40; 128 rows: 0.47, 0.57, 1.06, 2.0.)  Of seven
+// ways to cut, the least is taken: 128 users x 64 queries, a head of 64 over 800 keys 14.4 us unsplit and 30 in eights; over 3,000 keys of four
+// users 23.6 unsplit, 12 in eights.
+//
+// Partial results have room for PART_ROWS rows a compute unit and kernel: keys / chunk is rounded, by a third up at most where that makes two or
+// more, and tiles * keys / chunk <= work / chunk <= 3 / 4 of the room.
 static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays, CachePlan &plan, size_t &bytes)
 {
     const CacheShape &sh = c->shape;
@@ -399,27 +411,40 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         return (keys + CACHE_TILE - 1) / CACHE_TILE;
     };
     bytes = (size_t)n * sizeof(CacheAsk);
+    int64_t call_rows = 0;
+    for (int r = 0; r < n; ++r) call_rows += rows_of(asks[r]) * sh.n_kv;
+    const bool all_few = call_rows <= (int64_t)ROWS_OF_CU * c->n_cu;
     for (int kind = 0; kind < 2; ++kind) {
         CachePart &p = kind ? plan.many : plan.few;
-        auto mine = [&](const CacheAsk &a) { return a.n_q > 0 && (rows_of(a) > FEW_ROWS) == (kind == 1); };
+        auto mine = [&](const CacheAsk &a) { return a.n_q > 0 && (!all_few && rows_of(a) > FEW_ROWS) == (kind == 1); };
         int64_t most = 0, wide = 0;
+        bool windows = false;
         for (int r = 0; r < n; ++r)
-            if (mine(asks[r])) most = std::max(most, rows_of(asks[r])), wide += (rows_of(asks[r]) + 255) / 256 * sh.n_kv;
+            if (mine(asks[r])) most = std::max(most, rows_of(asks[r])), wide += (rows_of(asks[r]) + 255) / 256 * sh.n_kv, windows |= asks[r].pos && asks[r].window;
         if (most == 0) continue;
         const int rows = p.rows_of_tile = kind ? (sh.dtype == 1 && sh.dp <= 128 && wide >= 2 * c->n_cu ? 256 : 128) : (sh.dtype == 0 || most <= 16 ? 16 : 32);
-        // Heads of up to 32 features, and fp32 up to 64, are the cheapest to bring to bf16 once a wave (8 x 10^4 rows of 8 heads of 16 over 2,000 keys 255 us, 276
-        // once a block); up to 64 that also serves few row tiles, whose blocks wait for nobody, and rows that see each a window of its
-        // own, of which a wave's span less than a block's (replayed impressions 31 us, 48).
-        bool windows = false;
-        for (int r = 0; r < n; ++r) windows |= mine(asks[r]) && asks[r].pos && asks[r].window;
         p.own = kind && sh.dp <= 64 && (sh.dp == 32 || sh.dtype == 0 || rows == 128 || windows);
         const int64_t room = (int64_t)c->n_cu * PART_ROWS / rows;
         auto tiles_of = [&](const CacheAsk &a) { return (rows_of(a) + rows - 1) / rows; };
-        int64_t work = 0, all = 0, units = 0, joined = 0, parts = 0, most_units = 0;
+        int64_t work = 0, all = 0, valid = 0, longest = 0, units = 0, joined = 0, parts = 0, most_units = 0;
         for (int r = 0; r < n; ++r)
-            if (mine(asks[r])) work += tiles_of(asks[r]) * keys_of(asks[r], rows) * sh.n_kv, all += tiles_of(asks[r]) * sh.n_kv;
-        const int64_t blocks = std::min<int64_t>(room * 3 / 4, (int64_t)c->n_cu * (kind || sh.dp > 64 ? 2 : 4));      // a compute unit holds about so many
-        const int64_t chunk = std::max<int64_t>(kind && 4 * all < c->n_cu ? FEW_TILES : MIN_TILES, (work + blocks - 1) / blocks);
+            if (mine(asks[r])) {
+                const int64_t keys = keys_of(asks[r], rows);
+                work += tiles_of(asks[r]) * keys * sh.n_kv, all += tiles_of(asks[r]) * sh.n_kv, valid += rows_of(asks[r]) * sh.n_kv, longest = std::max(longest, keys);
+            }
+        const double tile = kind ? (0.1 + 0.0075 * sh.dp) * (sh.dtype == 0 ? 1.5 : 1.0) * (rows == 256 ? 1.7 : 1.0)
+                                 : (0.1 + 0.0012 * sh.dp) * (sh.dtype == 1 && rows == 16 ? 0.72 : 1.0);
+        const double row_of_part = sh.dp * 8 / 1.8e6;
+        int64_t chunk = std::max<int64_t>(longest, 1);
+        double best = tile * std::max((double)longest, 0.8 * work / all * ((all + c->n_cu - 1) / c->n_cu));
+        for (int m = 1; m <= 32; m *= 2) {                      // so many eighths of the compute units' number
+            const int64_t blocks = std::min<int64_t>(room * 3 / 4, (int64_t)c->n_cu * m / 8);
+            const int64_t k = std::max<int64_t>(MIN_TILES, (work + blocks - 1) / blocks);
+            if (k >= longest) continue;
+            const int64_t cut = std::max(all, work / k);
+            const double t = tile * std::max((double)k, 0.8 * work / cut * ((cut + c->n_cu - 1) / c->n_cu)) + 4.0 + row_of_part * valid * cut / all;
+            if (t < best) best = t, chunk = k;
+        }
         int32_t *first = arrays, *joins = arrays + n + 1;
         arrays += 2 * (n + 1);
         bytes += 2 * ((size_t)n + 1) * sizeof(int32_t);
