@@ -62,10 +62,10 @@ typedef struct {
     int32_t n_kv_heads;     /* heads of a key or value row                                           */
     int32_t d_head;         /* a multiple of 16 bytes in dtype, up to 256                            */
     float scale;            /* of the scores, > 0; 0 stands for 1 / sqrt(d_head)                     */
-    int32_t page_len;       /* rows of a page: a multiple of 32, 32..1024                            */
+    int32_t page_len;       /* rows of a page: a multiple of 32, 32..1024; a page has up to 2^29 bytes */
     int32_t n_pages;        /* pages of the pool                                                     */
     int32_t max_seqs;       /* sequence numbers are 0 .. max_seqs - 1                                */
-    int32_t max_len;        /* longest sequence, in rows                                             */
+    int32_t max_len;        /* longest sequence, in rows: up to 2^30, and 2^23 pages                 */
     int32_t max_requests;   /* entries of one call                                                   */
     int32_t max_queries;    /* largest n_q of one entry of aif_cache_attend                          */
 } aif_cache_config;
@@ -132,7 +132,8 @@ AIF_API aif_status aif_cache_append(aif_cache_ctx *ctx, const aif_cache_append_r
  * in bf16 the weights are rounded to bf16 where they meet the values.  What a query does not see does not reach it,
  * NaN included.  How a long sequence is shared out, and with it the order of the additions, depends on the call; the same call
  * gives the same bits.  The outputs must not overlap the pool, the queries or each other.
- * Errors: AIF_EINVAL, AIF_ERANGE. */
+ * Errors: AIF_EINVAL, AIF_ERANGE (a number outside the context; more than 2^31 - 1 queries times heads of a kv head in the
+ * call, or more than about 10^9 of them in large entries). */
 AIF_API aif_status aif_cache_attend(aif_cache_ctx *ctx, const aif_cache_attend_req *reqs, int32_t n, void *hip_stream);
 
 /* Unpacks rows.  Errors: AIF_EINVAL; AIF_ERANGE (rows at or beyond the sequence's length, or dropped by aif_cache_trim). */

@@ -739,7 +739,11 @@ class CacheContext:
         if n_pages is not None and n_pages > have:
             raise ValueError(f"the pool holds {have} pages, not {n_pages}")
         self._check(self._lib.aif_cache_swap_pool(self._h, _ptr(pool), have if n_pages is None else n_pages))
-        self._keep = self._keep + (pool,)          # the old pool may still be read by enqueued work
+        import torch
+        for old in self._keep:                     # enqueued work may still read it: its memory is not given away before that has run
+            if old.is_cuda:
+                old.record_stream(torch.cuda.current_stream())
+        self._keep = (pool,)
 
     def aif_cache_len(self, seq: int) -> int:
         return int(self._lib.aif_cache_len(self._h, seq))

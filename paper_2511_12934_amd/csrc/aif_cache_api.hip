@@ -18,7 +18,11 @@ using namespace aif;
 
 namespace {
 constexpr size_t CACHE_LIST_BYTES = 512 << 10;      // of one launch's descriptors, at most
-constexpr int FEW_ROWS = 64, ROWS_OF_CU = 64, MIN_TILES = 4, MAX_SPLITS = 128, PART_ROWS = 384;     // plan_attend
+constexpr int FEW_ROWS = 64, ROWS_OF_CU = 64, MIN_TILES = 4, MAX_SPLITS = 128, PART_ROWS = 384;      // plan_attend
+constexpr int MAX_UNITS = (1 << 23) - 1;    // of up to 512 threads: a grid holds fewer than 2^32 along an axis
+constexpr int CACHE_MAX_LEN = 1 << 30;      // row numbers and sums of two of them fit in 32 bits
+constexpr int CACHE_MAX_PAGES = 1 << 23;    // of a sequence, and
+constexpr size_t CACHE_MAX_PAGE = 1u << 29; // bytes of a page: a grid's second axis (k_cache_fill, k_cache_move) has up to 65,535 blocks
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
 }  // namespace
@@ -65,6 +69,11 @@ aif_status cfail(aif_cache_ctx *c, aif_status st, const char *fmt, ...)
                          hipGetErrorString(e_));                                                      \
     } while (0)
 
+size_t bytes_of_page(const aif_cache_config *f)
+{
+    return (size_t)f->n_kv_heads * (f->page_len / CACHE_TILE) * cache_tile_bytes((f->d_head + CACHE_BLOCK - 1) / CACHE_BLOCK * CACHE_BLOCK);
+}
+
 aif_status check_config(const aif_cache_config *f)
 {
     if (f->dtype != AIF_F32 && f->dtype != AIF_BF16) return cfail(nullptr, AIF_EINVAL, "unknown dtype %d", (int)f->dtype);
@@ -75,6 +84,7 @@ aif_status check_config(const aif_cache_config *f)
     if (f->d_head % vec || f->d_head > CACHE_MAX_DP) return cfail(nullptr, AIF_ESHAPE, "d_head %d is not a multiple of %d up to %d", f->d_head, vec, CACHE_MAX_DP);
     if (f->page_len < CACHE_TILE || f->page_len > 1024 || f->page_len % CACHE_TILE)
         return cfail(nullptr, AIF_ESHAPE, "page_len %d is not a multiple of %d up to 1024", f->page_len, CACHE_TILE);
+    if (bytes_of_page(f) > CACHE_MAX_PAGE) return cfail(nullptr, AIF_ESHAPE, "pages of %zu bytes are above %zu", bytes_of_page(f), CACHE_MAX_PAGE);
     return AIF_OK;
 }
 
@@ -215,6 +225,7 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     if (st != AIF_OK) return st;
     if (f->n_pages <= 0 || f->max_seqs <= 0 || f->max_len <= 0 || f->max_requests <= 0 || f->max_queries <= 0)
         return cfail(nullptr, AIF_EINVAL, "non-positive size in aif_cache_config");
+    if (f->max_len > CACHE_MAX_LEN) return cfail(nullptr, AIF_ESHAPE, "max_len %d is above %d", f->max_len, CACHE_MAX_LEN);
     if (f->max_requests > 65535) return cfail(nullptr, AIF_ESHAPE, "max_requests %d is above 65535", f->max_requests);
     if (!(f->scale >= 0.f) || f->scale - f->scale != 0.f) return cfail(nullptr, AIF_EINVAL, "scale is negative or not finite");
     if (!pool || (uintptr_t)pool % 64) return cfail(nullptr, AIF_EINVAL, "the pool is NULL or not 64-byte aligned");
@@ -239,6 +250,7 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     s.dtype = f->dtype == AIF_F32 ? 0 : 1;
     s.scale = f->scale != 0.f ? f->scale : 1.0f / __builtin_sqrtf((float)f->d_head);
     s.pages_per_seq = (int)(((int64_t)f->max_len + f->page_len - 1) / f->page_len);
+    if (s.pages_per_seq > CACHE_MAX_PAGES) return cfail(nullptr, AIF_ESHAPE, "max_len / page_len = %d pages of a sequence are above %d", s.pages_per_seq, CACHE_MAX_PAGES);
     const int64_t entries = (int64_t)f->max_seqs * s.pages_per_seq;
     if (entries > INT32_MAX / 2) return cfail(nullptr, AIF_ESHAPE, "max_seqs * max_len / page_len = %lld table entries are too many", (long long)entries);
     c->book.init(f->max_seqs, f->max_len, f->page_len, f->n_pages);
@@ -263,8 +275,7 @@ extern "C" {
 size_t aif_cache_page_bytes(const aif_cache_config *f)
 {
     if (!f || check_config(f) != AIF_OK) return 0;
-    const int dp = (f->d_head + CACHE_BLOCK - 1) / CACHE_BLOCK * CACHE_BLOCK;
-    return (size_t)f->n_kv_heads * (f->page_len / CACHE_TILE) * cache_tile_bytes(dp);
+    return bytes_of_page(f);
 }
 
 aif_status aif_cache_init(const aif_cache_config *cfg, void *pool, aif_cache_ctx **out)
@@ -462,7 +473,7 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
                 joined += rows_of(a);
                 parts += tiles * a.splits * sh.n_kv;
             }
-            if (units > INT32_MAX) return false;
+            if (units > MAX_UNITS) return false;
         }
         first[n] = (int32_t)units;
         joins[n] = (int32_t)joined;
@@ -492,9 +503,9 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
                           (st = check_tensor(c, "attend", r, q.out, q.out_stride, width)) != AIF_OK))
             return st;
         if (((uintptr_t)q.lse_out | (uintptr_t)q.positions) % 4) return cfail(c, AIF_EINVAL, "attend %d: lse_out and positions must be 4-byte aligned", r);
-        rows += q.n_q;
+        rows += (int64_t)q.n_q * c->shape.group;
     }
-    if (rows > INT32_MAX) return cfail(c, AIF_ERANGE, "%lld queries in one call are too many", (long long)rows);
+    if (rows > INT32_MAX) return cfail(c, AIF_ERANGE, "%lld rows (queries times heads of a kv head) in one call are too many", (long long)rows);
     hipStream_t s = (hipStream_t)hip_stream;
     if ((st = check_stream(c, s)) != AIF_OK) return st;
     if (rows == 0) return AIF_OK;
@@ -614,7 +625,9 @@ aif_status aif_cache_trim(aif_cache_ctx *c, const int32_t *seqs, int32_t n, int3
     hipStream_t s = (hipStream_t)hip_stream;
     if ((st = check_stream(c, s)) != AIF_OK) return st;
     CacheBatch<CacheFill> batch(c, (size_t)n, s);
-    auto go = [&](const CacheList &l) { return launch_cache_fill(c->shape, l, c->shape.pages_per_seq, s); };
+    int longest = 0;
+    for (int i = 0; i < n; ++i) longest = std::max(longest, c->book.pages(c->book.len(seqs[i])));
+    auto go = [&](const CacheList &l) { return launch_cache_fill(c->shape, l, longest, s); };
     for (int i = 0; i < n && st == AIF_OK; ++i) {
         int lo, hi;
         c->book.trim(seqs[i], sinks, window, lo, hi);

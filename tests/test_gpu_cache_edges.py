@@ -1,0 +1,103 @@
+"""The user cache where sizes and routes are the rare ones: pages beyond 4 GB, the copied descriptors, calls that are too large, pools that change."""
+import gc
+import weakref
+
+import numpy as np
+import pytest
+
+import cache_reference as ref
+from paper_2511_12934_amd import binding as B
+from paper_2511_12934_amd import workloads as wl
+
+from test_gpu_cache import _say, check_attend, dev, fill, make, read, rows
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def torch():
+    import torch
+    return torch
+
+
+def test_pages_beyond_four_gigabytes(torch):
+    _say("pages beyond 4 GB")
+    rng = np.random.default_rng(1)
+    shape = dict(dtype=B.AIF_BF16, n_heads=8, n_kv_heads=8, d_head=256, page_len=1024)
+    page = B.cache_page_bytes(**shape)
+    each = 64                                                   # pages of one of the long sequences
+    n = -(-(1 << 32) // (each * page)) + 1                      # so many of them lie before the one that is looked at
+    pool = torch.empty(((n * each + 2) * page,), dtype=torch.uint8, device="cuda")
+    ctx = B.CacheContext(pool=pool, max_seqs=n + 2, max_len=each * 1024, max_requests=4, max_queries=70, **shape)
+    ones = torch.ones((each * 1024, 8, 256), dtype=torch.bfloat16, device="cuda")
+    ctx.aif_cache_append([B.CacheAppend(0, ones, ones)])
+    ctx.aif_cache_copy([0] * (n - 1), list(range(1, n)))
+    del ones
+    k, v = rows(rng, 300, 8, 256, "bf16"), rows(rng, 300, 8, 256, "bf16")
+    fill(torch, ctx, "bf16", n, k, v)
+    assert ctx.aif_cache_free_pages() == 1
+    gk, gv = read(torch, ctx, "bf16", n, 8, 256)
+    assert np.array_equal(gk, ref.hold(k)) and np.array_equal(gv, ref.hold(v))
+    q = wl.round_storage(rng.standard_normal((70, 8, 256)).astype(np.float32), "bf16")
+    check_attend(torch, ctx, "bf16", n, k, v, q[:1], scale=1 / 16, what="one query")
+    check_attend(torch, ctx, "bf16", n, k, v, q, scale=1 / 16, what="70 queries")
+    ctx.aif_cache_copy([n], [n + 1])
+    ctx.aif_cache_free(list(range(n)))
+    assert ctx.aif_cache_compact() == 2
+    check_attend(torch, ctx, "bf16", n + 1, k, v, q[:3], scale=1 / 16, what="moved")
+    assert np.array_equal(read(torch, ctx, "bf16", n, 8, 256)[0], ref.hold(k))
+
+
+def test_descriptors_that_are_copied_to_the_device(torch, monkeypatch):
+    """The route of a host whose pinned memory is not mapped, with more descriptors than a launch's arguments hold."""
+    _say("descriptors by copy")
+    results = []
+    for copied in (False, True):
+        if copied:
+            monkeypatch.setenv("AIF_STAGING_COPY", "1")
+        rng = np.random.default_rng(2)
+        n = 150
+        ctx = make(torch, "bf16", 2, 1, 32, 32, pages=4 * n, seqs=2 * n, longest=100, requests=n, queries=4)
+        data = [rows(rng, int(m), 1, 32, "bf16") for m in rng.integers(0, 100, n)]
+        ctx.aif_cache_append([B.CacheAppend(u, dev(torch, x, "bf16"), dev(torch, x, "bf16")) for u, x in enumerate(data)])
+        some = list(range(0, n, 2))
+        ctx.aif_cache_fork(some, [n + u for u in some])
+        ctx.aif_cache_free(some)
+        q = dev(torch, rng.standard_normal((n, 2, 2, 32)), "bf16")
+        out = torch.full_like(q, float("nan"))
+        ctx.aif_cache_attend([B.CacheQuery(u + (n if u % 2 == 0 else 0), q[u], out[u]) for u in range(n)])
+        back = [torch.zeros((len(x), 1, 32), dtype=torch.bfloat16, device="cuda") for x in data]
+        ctx.aif_cache_read([B.CacheRead(u + (n if u % 2 == 0 else 0), b, None) for u, b in enumerate(back)])
+        torch.cuda.synchronize()
+        for b, x in zip(back, data):
+            assert np.array_equal(b.float().cpu().numpy(), ref.hold(x))
+        results.append(out.float().cpu().numpy())
+    assert np.array_equal(results[0], results[1])
+
+
+def test_calls_of_more_rows_than_their_numbers_reach_are_refused(torch):
+    _say("too many rows")
+    ctx = make(torch, "bf16", 4, 1, 64, requests=4, queries=2 ** 31 - 1)
+    q = torch.zeros((2, 4, 64), dtype=torch.bfloat16, device="cuda")
+    for n_q in (2 ** 29, 2 ** 30, 2 ** 31 - 1):
+        r = B.pack_cache_queries([B.CacheQuery(0, q, torch.empty_like(q))])
+        r[0].n_q = n_q
+        assert ctx._lib.aif_cache_attend(ctx._h, r, 1, None) == B.AIF_ERANGE
+        assert "too many" in ctx._lib.aif_cache_last_error(ctx._h).decode()
+
+
+def test_a_pool_that_was_left_is_not_kept(torch):
+    _say("pools that change")
+    rng = np.random.default_rng(3)
+    ctx = make(torch, "f32", 1, 1, 32, 32, pages=40, seqs=2, longest=600)
+    k = rows(rng, 600, 1, 32, "f32")
+    fill(torch, ctx, "f32", 0, k, k)
+    first = weakref.ref(ctx._keep[0])
+    assert ctx.aif_cache_compact() == 19
+    pool = torch.empty((19 * B.cache_page_bytes(dtype=B.AIF_F32, n_heads=1, n_kv_heads=1, d_head=32, page_len=32),), dtype=torch.uint8, device="cuda")
+    pool.copy_(ctx._keep[0][:pool.numel()])
+    ctx.aif_cache_swap_pool(pool)
+    gc.collect()
+    assert first() is None
+    q = wl.round_storage(rng.standard_normal((5, 1, 32)).astype(np.float32), "f32")
+    check_attend(torch, ctx, "f32", 0, k, k, q, scale=32 ** -0.5, what="the new pool")
