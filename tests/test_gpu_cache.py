@@ -334,8 +334,9 @@ def test_branches_share_pages_until_they_are_written(torch):
     page = B.cache_page_bytes(dtype=B.AIF_BF16, n_heads=heads, n_kv_heads=kv, d_head=d, page_len=pl)
     smaller = torch.full(((used + 2) * page,), 0xff, dtype=torch.uint8, device="cuda")
     smaller[:used * page] = ctx._keep[0][:used * page]
+    old = ctx._keep[0]
     ctx.aif_cache_swap_pool(smaller)
-    ctx._keep[0].fill_(0xff)
+    old.fill_(0xff)
     assert ctx.aif_cache_free_pages() == 2
     check(drop)
     put((8,), 33)
