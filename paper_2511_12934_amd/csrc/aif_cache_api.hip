@@ -25,6 +25,7 @@ constexpr int CACHE_MAX_PAGES = 1 << 23;    // of a sequence, and
 constexpr size_t CACHE_MAX_PAGE = 1u << 29; // bytes of a page: a grid's second axis (k_cache_fill, k_cache_move) has up to 65,535 blocks
 constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
+constexpr int LEAN_ASKS = (CACHE_FEW_BYTES - sizeof(CacheLean) - 2 * sizeof(int32_t)) / (sizeof(CacheOwn) + 2 * sizeof(int32_t));     // that fit with one kernel's numbers
 }  // namespace
 
 struct aif_cache_ctx {
@@ -45,6 +46,7 @@ struct aif_cache_ctx {
     hipEvent_t ev[2] = {};
     bool ev_live[2] = {};
     alignas(16) char few[CACHE_FEW_BYTES];
+    alignas(16) char lean[LEAN_ASKS * sizeof(CacheAsk) + 4 * (LEAN_ASKS + 1) * sizeof(int32_t)];      // asks before they go into `few`
     char err[512] = "";
 };
 
@@ -487,6 +489,20 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
     return true;
 }
 
+// Whether entries differ in nothing but their sequences and evenly spaced pointers.
+static bool alike(const aif_cache_attend_req *q, int32_t n)
+{
+    for (int r = 1; r < n; ++r) {
+        const aif_cache_attend_req &a = q[r], &b = q[r - 1], &z = q[0], &o = q[1];
+        auto even = [](const void *x, const void *y, const void *first, const void *second) { return (uintptr_t)x - (uintptr_t)y == (uintptr_t)second - (uintptr_t)first; };
+        if (a.n_q != z.n_q || a.q_stride != z.q_stride || a.out_stride != z.out_stride || a.sinks != z.sinks || a.window != z.window ||
+            !a.lse_out != !z.lse_out || !a.positions != !z.positions || !even(a.q, b.q, z.q, o.q) || !even(a.out, b.out, z.out, o.out) ||
+            !even(a.lse_out, b.lse_out, z.lse_out, o.lse_out) || !even(a.positions, b.positions, z.positions, o.positions))
+            return false;
+    }
+    return true;
+}
+
 aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, int32_t n, void *hip_stream)
 {
     if (!c) return AIF_EINVAL;
@@ -510,11 +526,13 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
     if ((st = check_stream(c, s)) != AIF_OK) return st;
     if (rows == 0) return AIF_OK;
 
-    const bool far = attend_bytes((size_t)n) > CACHE_FEW_BYTES;
+    // The descriptors go into the arguments as they are; or as what they have in common and what they have not; or are uploaded.
+    bool far = attend_bytes((size_t)n) > CACHE_FEW_BYTES;
+    const bool lean = far && n <= LEAN_ASKS && alike(reqs, n);
     size_t bytes = 0;
     size_t off = 0;
-    char *h = c->few;
-    if (far) {
+    char *h = lean ? c->lean : c->few;
+    if (far && !lean) {
         if ((st = stage_take(c, attend_bytes((size_t)n), s, off)) != AIF_OK) return st;
         h = c->h_stage + off;
     }
@@ -527,6 +545,22 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
     CachePlan plan{};
     if (!plan_attend(c, ha, n, (int32_t *)(ha + n), plan, bytes)) return cfail(c, AIF_ERANGE, "one call has too many queries");
     CacheList l{h, nullptr, n, bytes};
+    if (lean) {
+        const size_t numbers = bytes - n * sizeof(CacheAsk), asks = cache_asks_bytes(n, true);
+        far = asks + numbers > CACHE_FEW_BYTES;
+        if (far) {
+            if ((st = stage_take(c, bytes, s, off)) != AIF_OK) return st;
+            __builtin_memcpy(c->h_stage + off, h, bytes);
+        } else {
+            auto step = [&](auto f) { return n > 1 ? (int64_t)((uintptr_t)f(ha[1]) - (uintptr_t)f(ha[0])) : 0; };
+            *(CacheLean *)c->few = CacheLean{ha[0], step([](const CacheAsk &a) { return a.q; }), step([](const CacheAsk &a) { return a.out; }),
+                                             step([](const CacheAsk &a) { return a.lse; }), step([](const CacheAsk &a) { return a.pos; })};
+            CacheOwn *own = (CacheOwn *)(c->few + sizeof(CacheLean));
+            for (int r = 0; r < n; ++r) own[r] = CacheOwn{ha[r].len, ha[r].entry, ha[r].splits, ha[r].part};
+            __builtin_memcpy(c->few + asks, ha + n, numbers);
+            l = CacheList{c->few, nullptr, n, asks + numbers, true};
+        }
+    }
     if (far) {
         CACHE_TRY(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
         l.dev = c->d_stage + off;

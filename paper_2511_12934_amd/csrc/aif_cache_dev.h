@@ -56,6 +56,16 @@ struct CacheAsk {
     int32_t pad_;
 };
 
+// Entries that differ in their sequence and in what a step from one to the next makes of their pointers (a batch's queries and outputs lie in one
+// tensor): entry 0's ask, the steps in bytes, and for each entry what it has of its own.
+struct CacheLean {
+    CacheAsk a;
+    int64_t q_step, out_step, lse_step, pos_step;
+};
+struct CacheOwn {
+    int32_t len, entry, splits, part;
+};
+
 // Descriptors of a launch.  Few of them travel in the kernel's arguments (which hold 4 KB), more are uploaded.
 constexpr int CACHE_FEW_BYTES = 3456;
 struct CacheFew {
@@ -69,7 +79,9 @@ struct CacheList {
     const char *dev;            // where they are on the device, or null: in the arguments
     int32_t n;
     size_t bytes;
+    bool lean = false;          // asks: CacheLean, CacheOwn[n] in the place of CacheAsk[n]
 };
+inline size_t cache_asks_bytes(int n, bool lean) { return lean ? sizeof(CacheLean) + n * sizeof(CacheOwn) : n * sizeof(CacheAsk); }
 
 hipError_t launch_cache_append(const CacheShape &c, const CacheList &units, hipStream_t s);
 hipError_t launch_cache_read(const CacheShape &c, const CacheList &units, hipStream_t s);
@@ -77,7 +89,7 @@ hipError_t launch_cache_fill(const CacheShape &c, const CacheList &fills, int lo
 hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStream_t s);
 
 // Attention.  A row is a query and one of the `group` heads that share a kv head; a unit is a tile of rows and one of the splits of
-// its keys.  An entry of few rows goes to one kernel, one of many to another.  asks: n CacheAsk, then for each of the two kernels that
+// its keys.  An entry of few rows goes to one kernel, one of many to another.  asks: cache_asks_bytes() of entries, then for each of the two kernels that
 // has any (few first) int32 first[n + 1], running numbers of units, and int32 joins[n + 1], running numbers of the rows whose keys are split.
 struct CachePart {
     int32_t units, joins;       // of all asks

@@ -19,6 +19,7 @@ constexpr float LOG2E = 1.44269504088896340736f, LN2 = 0.69314718055994530942f;
 struct CacheGrid {
     int32_t n, firsts;          // asks; byte offset of int32 first[n + 1]
     int32_t each;               // CachePart::each
+    int32_t lean;               // CacheList::lean
 };
 
 inline dim3 cache_grid(const CacheGrid &g, const CacheShape &c, const CachePart &p) { return p.each ? dim3(g.n, c.n_kv, p.each) : dim3(p.units, c.n_kv, 1); }
@@ -26,8 +27,19 @@ inline dim3 cache_grid(const CacheGrid &g, const CacheShape &c, const CachePart 
 void launch_cache_own(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
 void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
 
-__device__ __forceinline__ CacheAsk ask_at(const char *dev, int r)
+__device__ __forceinline__ CacheAsk ask_at(const char *dev, const CacheGrid &g, int r)
 {
+    if (g.lean) {               // (in the arguments)
+        const CacheLean l = arg_copy(kernel_arg<CacheLean>(0));
+        const CacheOwn o = arg_copy(kernel_arg<CacheOwn>(sizeof(CacheLean) + (size_t)r * sizeof(CacheOwn)));
+        CacheAsk a = l.a;
+        a.q += r * l.q_step;
+        a.out += r * l.out_step;
+        a.lse = (float *)((char *)a.lse + r * l.lse_step);
+        a.pos = (const int32_t *)((const char *)a.pos + r * l.pos_step);
+        a.len = o.len, a.entry = o.entry, a.splits = o.splits, a.part = o.part;
+        return a;
+    }
     const size_t off = (size_t)r * sizeof(CacheAsk);
     return dev ? *(const CacheAsk *)(as_global(dev) + off) : arg_copy(kernel_arg<CacheAsk>(off));
 }
@@ -58,12 +70,12 @@ __device__ __forceinline__ AskUnit block_ask(const char *dev, const CacheGrid &g
 {
     AskUnit u;
     if (g.each) {
-        u.a = ask_at(dev, blockIdx.x);
+        u.a = ask_at(dev, g, blockIdx.x);
         u.unit = blockIdx.z;
         return u;
     }
     const int r = ask_of(dev, g, blockIdx.x, lane);
-    u.a = ask_at(dev, r);
+    u.a = ask_at(dev, g, r);
     u.unit = (int)blockIdx.x - first_at(dev, g, r);
     return u;
 }

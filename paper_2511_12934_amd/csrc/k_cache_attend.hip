@@ -338,7 +338,7 @@ template <int DT> __global__ __launch_bounds__(128) void k_cache_join(CacheFew f
     (void)few;
     const int lane = threadIdx.x & 63, kvh = blockIdx.y;
     const int r = ask_of(dev, g, blockIdx.x, lane);
-    const CacheAsk a = ask_at(dev, r);
+    const CacheAsk a = ask_at(dev, g, r);
     const int row = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group, tiles = (n_rows + rows_of_tile - 1) / rows_of_tile;
     const size_t each = cache_part_floats(rows_of_tile, c.dp);
     const float *p = as_global(part) + ((size_t)a.part + ((size_t)kvh * tiles + row / rows_of_tile) * a.splits) * each;
@@ -422,7 +422,7 @@ hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const
 {
     CacheFew args;
     if (!asks.dev) __builtin_memcpy(args.w, asks.host, asks.bytes);
-    CacheGrid g{asks.n, (int32_t)(asks.n * sizeof(CacheAsk)), 0};
+    CacheGrid g{asks.n, (int32_t)cache_asks_bytes(asks.n, asks.lean), 0, asks.lean};
     for (int kind = 0; kind < 2; ++kind) {
         const CachePart &of = kind ? p.many : p.few;
         if (of.units == 0) continue;

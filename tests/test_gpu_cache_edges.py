@@ -9,7 +9,7 @@ import cache_reference as ref
 from paper_2511_12934_amd import binding as B
 from paper_2511_12934_amd import workloads as wl
 
-from test_gpu_cache import _say, check_attend, dev, fill, make, read, rows
+from test_gpu_cache import _say, check_attend, compare, dev, fill, make, read, rows
 
 pytestmark = pytest.mark.gpu
 
@@ -101,3 +101,36 @@ def test_a_pool_that_was_left_is_not_kept(torch):
     assert first() is None
     q = wl.round_storage(rng.standard_normal((5, 1, 32)).astype(np.float32), "f32")
     check_attend(torch, ctx, "f32", 0, k, k, q, scale=32 ** -0.5, what="the new pool")
+
+
+@pytest.mark.parametrize("n,n_q,longest", [(40, 1, 3000), (139, 1, 3000), (140, 1, 400), (100, 70, 200), (100, 300, 200), (300, 2, 100)])
+@pytest.mark.parametrize("window", (0, 90))
+def test_entries_alike_and_not_give_the_same_bits(torch, n, n_q, longest, window):
+    """Queries and outputs of a batch in one tensor each, and the same with one entry's output elsewhere."""
+    _say(f"{n} entries alike, {n_q} queries, window {window}")
+    rng = np.random.default_rng(n + n_q)
+    heads, kv, d = 4, 2, 64
+    ctx = make(torch, "bf16", heads, kv, d, 64, pages=n * (longest // 64 + 1), seqs=n, longest=longest, requests=n, queries=n_q)
+    source = dev(torch, rows(rng, longest, kv, d, "bf16"), "bf16")
+    lens = rng.integers(0, longest + 1, n)
+    lens[n - 1] = longest
+    ctx.aif_cache_append([B.CacheAppend(u, source[longest - m:], source[longest - m:]) for u, m in enumerate(lens)])
+    q_host = wl.round_storage(rng.standard_normal((n, n_q, heads, d)).astype(np.float32), "bf16")
+    q = dev(torch, q_host, "bf16")
+    where = rng.integers(-1, longest, (n, n_q)).astype(np.int32)
+    at = torch.from_numpy(where).cuda()
+    got = []
+    for apart in (False, True):
+        out, lse = torch.full_like(q, float("nan")), torch.full((n, n_q, heads), float("nan"), device="cuda")
+        outs = [out[u] for u in range(n)]
+        if apart:
+            outs[n // 2] = torch.full_like(q[0], float("nan"))
+        ctx.aif_cache_attend([B.CacheQuery(u, q[u], outs[u], lse=lse[u], positions=at[u] if window else None, window=window, sinks=3) for u in range(n)])
+        torch.cuda.synchronize()
+        got.append((torch.stack(outs).float().cpu().numpy(), lse.cpu().numpy()))
+    assert np.array_equal(got[0][0], got[1][0]) and np.array_equal(got[0][1], got[1][1])
+    held = source.float().cpu().numpy()
+    some = slice(0, 4)
+    for u in (0, n // 2, n - 1):
+        k = held[longest - lens[u]:]
+        compare("bf16", got[0][0][u][some], got[0][1][u][some], q_host[u][some], k, k, d ** -0.5, positions=where[u][some] if window else None, sinks=3, window=window, what=f"entry {u}")
