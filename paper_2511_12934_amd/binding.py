@@ -187,7 +187,8 @@ def _ptr(t) -> Optional[int]:
 
 def _stream() -> Optional[int]:
     import torch
-    return torch.cuda.current_stream().cuda_stream or None
+    # the handle itself: the Stream object around it takes 2.9 us a call, as much as a launch
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
 
 
 class Request:
