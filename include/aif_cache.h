@@ -136,7 +136,8 @@ AIF_API aif_status aif_cache_append(aif_cache_ctx *ctx, const aif_cache_append_r
  * call, or more than about 10^9 of them in large entries). */
 AIF_API aif_status aif_cache_attend(aif_cache_ctx *ctx, const aif_cache_attend_req *reqs, int32_t n, void *hip_stream);
 
-/* Unpacks rows.  Errors: AIF_EINVAL; AIF_ERANGE (rows at or beyond the sequence's length, or dropped by aif_cache_trim). */
+/* Unpacks rows.  Errors: AIF_EINVAL; AIF_ERANGE (rows at or beyond the sequence's length, or dropped by aif_cache_trim;
+ * more than about 10^9 rows in a call). */
 AIF_API aif_status aif_cache_read(aif_cache_ctx *ctx, const aif_cache_read_req *reqs, int32_t n, void *hip_stream);
 
 /* src, dst: HOST arrays of n sequence numbers.  dst[i], which must be empty and named once, becomes what src[i] is, sharing

@@ -23,7 +23,6 @@ constexpr int MAX_UNITS = (1 << 23) - 1;    // of up to 512 threads: a grid hold
 constexpr int CACHE_MAX_LEN = 1 << 30;      // row numbers and sums of two of them fit in 32 bits
 constexpr int CACHE_MAX_PAGES = 1 << 23;    // of a sequence, and
 constexpr size_t CACHE_MAX_PAGE = 1u << 29; // bytes of a page: a grid's second axis (k_cache_fill, k_cache_move) has up to 65,535 blocks
-constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
 thread_local char g_cache_init_error[512] = "";
 constexpr int LEAN_ASKS = (CACHE_FEW_BYTES - sizeof(CacheLean) - 2 * sizeof(int32_t)) / (sizeof(CacheOwn) + 2 * sizeof(int32_t));     // that fit with one kernel's numbers
 }  // namespace
@@ -47,11 +46,13 @@ struct aif_cache_ctx {
     bool ev_live[2] = {};
     alignas(16) char few[CACHE_FEW_BYTES];
     alignas(16) char lean[LEAN_ASKS * sizeof(CacheAsk) + 4 * (LEAN_ASKS + 1) * sizeof(int32_t)];      // asks before they go into `few`
+    std::vector<char> list;                 // a list before it goes into a launch's arguments or to the device
     char err[512] = "";
 };
 
 namespace {
 
+size_t outs_bytes(size_t n) { return n * sizeof(CacheOut) + (n + 1) * sizeof(int32_t); }
 size_t attend_bytes(size_t n) { return n * sizeof(CacheAsk) + 4 * (n + 1) * sizeof(int32_t); }
 
 aif_status cfail(aif_cache_ctx *c, aif_status st, const char *fmt, ...)
@@ -160,7 +161,7 @@ aif_status stage_take(aif_cache_ctx *c, size_t bytes, hipStream_t s, size_t &off
 }
 
 // A list of descriptors on its way to a launch.  Up to CACHE_FEW_BYTES of a call travel in the kernel's arguments; more are
-// cut into lists in pinned memory.
+// cut into lists in pinned memory, where the blocks read them.
 template <class T> class CacheBatch {
 public:
     CacheBatch(aif_cache_ctx *c, size_t expected, hipStream_t s) : c_(c), s_(s), far_(expected * sizeof(T) > CACHE_FEW_BYTES)
@@ -206,6 +207,63 @@ private:
     size_t room_, off_ = 0;
     T *at_ = nullptr;
     int n_ = 0;
+};
+
+// A list of which blocks look for their entry: in the arguments, or on the device.
+template <class F> aif_status send_list(aif_cache_ctx *c, const char *h, int n, size_t bytes, hipStream_t s, F &&go)
+{
+    CacheList l{h, nullptr, n, bytes};
+    if (bytes > CACHE_FEW_BYTES) {
+        size_t off = 0;
+        const aif_status st = stage_take(c, bytes, s, off);
+        if (st != AIF_OK) return st;
+        __builtin_memcpy(c->h_stage + off, h, bytes);
+        CACHE_TRY(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
+        l.dev = c->d_stage + off;
+    }
+    CACHE_TRY(c, go(l));
+    return AIF_OK;
+}
+
+// Pages that are copied, as runs of new ones that follow each other.
+class CacheCopies {
+public:
+    CacheCopies(aif_cache_ctx *c, hipStream_t s) : c_(c), s_(s), runs_((CacheRun *)c->list.data()) {}
+    aif_status add(int32_t src, int32_t dst, int32_t page)      // table entries, the new page (-1: none)
+    {
+        if (n_ && pages_ < MAX_UNITS) {
+            CacheRun &r = runs_[n_ - 1];
+            if (src == r.src + r.n && dst == r.dst + r.n && (page < 0 ? r.page < 0 : r.page >= 0 && page == r.page + r.n)) {
+                ++r.n, ++pages_;
+                return AIF_OK;
+            }
+        }
+        if (n_ == ROOM || pages_ == MAX_UNITS) {
+            const aif_status st = send();
+            if (st != AIF_OK) return st;
+        }
+        runs_[n_++] = CacheRun{src, dst, page, 1};
+        ++pages_;
+        return AIF_OK;
+    }
+    aif_status send()
+    {
+        if (n_ == 0) return AIF_OK;
+        int32_t *first = (int32_t *)(runs_ + n_);
+        const int n = n_, pages = pages_;
+        for (int i = 0, at = 0; i < n; at += runs_[i++].n) first[i] = at;
+        first[n] = pages;
+        n_ = pages_ = 0;
+        return send_list(c_, (const char *)runs_, n, n * sizeof(CacheRun) + (n + 1) * sizeof(int32_t), s_,
+                         [&](const CacheList &l) { return launch_cache_copy(c_->shape, l, pages, s_); });
+    }
+
+private:
+    static constexpr int ROOM = CACHE_LIST_BYTES / (sizeof(CacheRun) + sizeof(int32_t)) - 1;
+    aif_cache_ctx *c_;
+    hipStream_t s_;
+    CacheRun *runs_;
+    int n_ = 0, pages_ = 0;
 };
 
 void cdestroy(aif_cache_ctx *c)
@@ -263,6 +321,7 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     CACHE_TRY(nullptr, hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device));
     if (n_cu > 0) c->n_cu = n_cu;
     for (float *&p : c->part) CACHE_TRY(nullptr, hipMalloc((void **)&p, cache_part_floats(c->n_cu * PART_ROWS, s.dp) * sizeof(float)));
+    c->list.resize(std::max(CACHE_LIST_BYTES, outs_bytes(f->max_requests)));
     c->half_bytes = (std::max(2 * CACHE_LIST_BYTES, 4 * attend_bytes(f->max_requests)) + 255) / 256 * 256;        // (a list of asks is one, whatever its length)
     CACHE_TRY(nullptr, staging_alloc(c->half_bytes * 2, &c->h_stage, &c->h_stage_dev));
     CACHE_TRY(nullptr, hipMalloc((void **)&c->d_stage, c->half_bytes * 2));
@@ -359,6 +418,7 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
     if (st != AIF_OK) return st;
     const int width = c->shape.n_kv * c->shape.d_head, pl = c->cfg.page_len;
     int64_t units = 0;
+    int n_out = 0;
     for (int r = 0; r < n; ++r) {
         const aif_cache_read_req &q = reqs[r];
         if ((st = check_seq(c, "read", r, q.seq)) != AIF_OK) return st;
@@ -371,27 +431,26 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
             return st;
         for (int p = q.first / pl; p <= (q.first + q.n_rows - 1) / pl; ++p)
             if (c->book.page(q.seq, p) < 0) return cfail(c, AIF_ERANGE, "read %d: rows from %d on were dropped", r, p * pl);
-        units += runs_of(q.n_rows, pl);
+        if (!q.keys_out && !q.vals_out) continue;
+        units += unit_of_row(q.first + q.n_rows - 1, pl) - unit_of_row(q.first, pl) + 1;
+        ++n_out;
     }
+    if (units > 2 * MAX_UNITS) return cfail(c, AIF_ERANGE, "rows in %lld pieces of pages in one call are too many", (long long)units);
     hipStream_t s = (hipStream_t)hip_stream;
     if ((st = check_stream(c, s)) != AIF_OK) return st;
-    CacheBatch<CacheUnit> batch(c, (size_t)units, s);
-    auto go = [&](const CacheList &l) { return launch_cache_read(c->shape, l, s); };
-    const int esz = c->shape.dtype == 0 ? 4 : 2;
+    CacheOut *out = (CacheOut *)c->list.data();
+    int32_t *first = (int32_t *)(out + n_out), at = 0;
     for (int r = 0; r < n; ++r) {
         const aif_cache_read_req &q = reqs[r];
-        const int64_t ks = q.key_stride ? q.key_stride : width, vs = q.val_stride ? q.val_stride : width;
-        if (!q.keys_out && !q.vals_out) continue;
-        for (int done = 0; done < q.n_rows;) {
-            const int at = q.first + done, row0 = at % pl;
-            const int rows = std::min({UNIT_ROWS - row0 % UNIT_ROWS, pl - row0, q.n_rows - done});
-            const CacheUnit u{q.keys_out ? (const char *)q.keys_out + done * ks * esz : nullptr,
-                              q.vals_out ? (const char *)q.vals_out + done * vs * esz : nullptr, ks, vs, c->book.page(q.seq, at / pl), -1, row0, rows, 0, 0};
-            done += rows;
-            if ((st = batch.add(u, go)) != AIF_OK) return st;
-        }
+        if (q.n_rows == 0 || (!q.keys_out && !q.vals_out)) continue;
+        *first++ = at;
+        *out++ = CacheOut{(char *)q.keys_out, (char *)q.vals_out, q.key_stride ? q.key_stride : width, q.val_stride ? q.val_stride : width,
+                          c->book.entry(q.seq, 0), q.first, q.n_rows, 0};
+        at += unit_of_row(q.first + q.n_rows - 1, pl) - unit_of_row(q.first, pl) + 1;
     }
-    return batch.send(go);
+    *first = at;
+    if (n_out == 0) return AIF_OK;
+    return send_list(c, c->list.data(), n_out, outs_bytes(n_out), s, [&](const CacheList &l) { return launch_cache_read(c->shape, l, at, s); });
 }
 
 // How a call's work is cut: into tiles of rows (a row is a query and a head of a kv head's group) and, where that pays, splits of their keys.
@@ -610,21 +669,17 @@ aif_status aif_cache_copy(aif_cache_ctx *c, const int32_t *src, const int32_t *d
     if (!c) return AIF_EINVAL;
     aif_status st = check_branches(c, "copy", src, dst, n);
     if (st != AIF_OK) return st;
-    int64_t pages = 0, entries = 0;
-    for (int i = 0; i < n; ++i) {
-        pages += c->book.copy_needs(src[i]);
-        entries += c->book.pages(c->book.len(src[i]));
-    }
+    int64_t pages = 0;
+    for (int i = 0; i < n; ++i) pages += c->book.copy_needs(src[i]);
     if (pages > c->book.n_free) return cfail(c, AIF_ERANGE, "%lld pages needed, %d are free", (long long)pages, c->book.n_free);
     hipStream_t s = (hipStream_t)hip_stream;
     if ((st = check_stream(c, s)) != AIF_OK) return st;
-    CacheBatch<CacheMove> batch(c, (size_t)entries, s);
-    auto go = [&](const CacheList &l) { return launch_cache_move(c->shape, l, s); };
+    CacheCopies copies(c, s);
     for (int i = 0; i < n && st == AIF_OK; ++i)
-        c->book.copy(src[i], dst[i], [&](int32_t p, int32_t from, int32_t to) {
-            if (st == AIF_OK) st = batch.add(CacheMove{from, to, c->book.entry(dst[i], p)}, go);
+        c->book.copy(src[i], dst[i], [&](int32_t p, int32_t, int32_t to) {
+            if (st == AIF_OK) st = copies.add(c->book.entry(src[i], p), c->book.entry(dst[i], p), to);
         });
-    return st == AIF_OK ? batch.send(go) : st;
+    return st == AIF_OK ? copies.send() : st;
 }
 
 aif_status aif_cache_free(aif_cache_ctx *c, const int32_t *seqs, int32_t n)

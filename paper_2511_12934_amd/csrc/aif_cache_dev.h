@@ -35,6 +35,17 @@ struct CacheUnit {
     int32_t row0, n;
     int32_t entry, pad_;        // the table entry that names the page
 };
+// Rows [first, first + n) of a sequence whose table entries start at `entry`, to keys and vals (or null; strides in elements).
+struct CacheOut {
+    char *keys, *vals;
+    int64_t key_stride, val_stride;
+    int32_t entry, first, n, pad_;
+};
+// Pages of a sequence copied to new ones that follow each other: those that table entries [src, src + n) name become the pages from `page` on, and
+// entries [dst, dst + n) name them.  page < 0: the entries become -1.
+struct CacheRun {
+    int32_t src, dst, page, n;
+};
 // Table entries [dst, dst + n): those at src, or `value` where src < 0.
 struct CacheFill {
     int32_t dst, n, src, value;
@@ -84,9 +95,15 @@ struct CacheList {
 inline size_t cache_asks_bytes(int n, bool lean) { return lean ? sizeof(CacheLean) + n * sizeof(CacheOwn) : n * sizeof(CacheAsk); }
 
 hipError_t launch_cache_append(const CacheShape &c, const CacheList &units, hipStream_t s);
-hipError_t launch_cache_read(const CacheShape &c, const CacheList &units, hipStream_t s);
+// outs: n CacheOut, then int32 first[n + 1], running numbers of their units (see unit_of_row); runs: n CacheRun, then those of their pages.
+hipError_t launch_cache_read(const CacheShape &c, const CacheList &outs, int units, hipStream_t s);
+hipError_t launch_cache_copy(const CacheShape &c, const CacheList &runs, int pages, hipStream_t s);
 hipError_t launch_cache_fill(const CacheShape &c, const CacheList &fills, int longest, hipStream_t s);
 hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStream_t s);
+
+constexpr int UNIT_ROWS = 64;               // rows of a page that one block of the append and read kernels takes
+// the unit that a row of a sequence lies in: a page's rows in pieces of UNIT_ROWS, the last one shorter
+__host__ __device__ inline int unit_of_row(int row, int page_len) { return row / page_len * ((page_len + UNIT_ROWS - 1) / UNIT_ROWS) + row % page_len / UNIT_ROWS; }
 
 // Attention.  A row is a query and one of the `group` heads that share a kv head; a unit is a tile of rows and one of the splits of
 // its keys.  An entry of few rows goes to one kernel, one of many to another.  asks: cache_asks_bytes() of entries, then for each of the two kernels that
@@ -108,6 +125,28 @@ hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const
 template <class T> __device__ __forceinline__ T cache_desc(const CacheFew &, size_t off) { return arg_copy(kernel_arg<T>(off)); }
 template <class T> __device__ __forceinline__ T cache_desc(const CacheFar &far, size_t off) { return *(const T *)(as_global(far.dev) + off); }
 
+template <class T> __device__ __forceinline__ T desc_at(const char *dev, int i)
+{
+    return dev ? *(const T *)(as_global(dev) + (size_t)i * sizeof(T)) : arg_copy(kernel_arg<T>((size_t)i * sizeof(T)));
+}
+__device__ __forceinline__ int first_at(const char *dev, int firsts, int i)
+{
+    const size_t off = (size_t)firsts + 4 * (size_t)i;
+    return dev ? *(const int32_t *)(as_global(dev) + off) : *kernel_arg<int32_t>(off);
+}
+// The entry that a unit belongs to, by running numbers int32 first[n + 1] at byte `firsts` of the descriptors: 64 of them at a time.
+__device__ __forceinline__ int entry_of(const char *dev, int n, int firsts, int unit, int lane)
+{
+    int r = 0;
+    for (int base = 1; base <= n; base += 64) {
+        const int i = base + lane;
+        const int f = first_at(dev, firsts, i <= n ? i : n);
+        const int below = __popcll(__ballot(i <= n && f <= unit));
+        r += below;
+        if (below < 64) break;
+    }
+    return __builtin_amdgcn_readfirstlane(r);
+}
 template <class F> hipError_t cache_launch(const CacheList &list, F &&go)
 {
     if (list.dev) {

@@ -40,26 +40,7 @@ __device__ __forceinline__ CacheAsk ask_at(const char *dev, const CacheGrid &g, 
         a.len = o.len, a.entry = o.entry, a.splits = o.splits, a.part = o.part;
         return a;
     }
-    const size_t off = (size_t)r * sizeof(CacheAsk);
-    return dev ? *(const CacheAsk *)(as_global(dev) + off) : arg_copy(kernel_arg<CacheAsk>(off));
-}
-__device__ __forceinline__ int first_at(const char *dev, const CacheGrid &g, int i)
-{
-    const size_t off = (size_t)g.firsts + 4 * (size_t)i;
-    return dev ? *(const int32_t *)(as_global(dev) + off) : *kernel_arg<int32_t>(off);
-}
-// The ask that a unit belongs to: 64 running numbers at a time.
-__device__ __forceinline__ int ask_of(const char *dev, const CacheGrid &g, int unit, int lane)
-{
-    int r = 0;
-    for (int base = 1; base <= g.n; base += 64) {
-        const int i = base + lane;
-        const int f = first_at(dev, g, i <= g.n ? i : g.n);
-        const int below = __popcll(__ballot(i <= g.n && f <= unit));
-        r += below;
-        if (below < 64) break;
-    }
-    return __builtin_amdgcn_readfirstlane(r);
+    return desc_at<CacheAsk>(dev, r);
 }
 // The block's ask and its unit of it.
 struct AskUnit {
@@ -74,9 +55,9 @@ __device__ __forceinline__ AskUnit block_ask(const char *dev, const CacheGrid &g
         u.unit = blockIdx.z;
         return u;
     }
-    const int r = ask_of(dev, g, blockIdx.x, lane);
+    const int r = entry_of(dev, g.n, g.firsts, blockIdx.x, lane);
     u.a = ask_at(dev, g, r);
-    u.unit = (int)blockIdx.x - first_at(dev, g, r);
+    u.unit = (int)blockIdx.x - first_at(dev, g.firsts, r);
     return u;
 }
 

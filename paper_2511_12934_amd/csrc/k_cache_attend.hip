@@ -337,9 +337,9 @@ template <int DT> __global__ __launch_bounds__(128) void k_cache_join(CacheFew f
 {
     (void)few;
     const int lane = threadIdx.x & 63, kvh = blockIdx.y;
-    const int r = ask_of(dev, g, blockIdx.x, lane);
+    const int r = entry_of(dev, g.n, g.firsts, blockIdx.x, lane);
     const CacheAsk a = ask_at(dev, g, r);
-    const int row = (int)blockIdx.x - first_at(dev, g, r), n_rows = a.n_q * c.group, tiles = (n_rows + rows_of_tile - 1) / rows_of_tile;
+    const int row = (int)blockIdx.x - first_at(dev, g.firsts, r), n_rows = a.n_q * c.group, tiles = (n_rows + rows_of_tile - 1) / rows_of_tile;
     const size_t each = cache_part_floats(rows_of_tile, c.dp);
     const float *p = as_global(part) + ((size_t)a.part + ((size_t)kvh * tiles + row / rows_of_tile) * a.splits) * each;
     const int cl = row % rows_of_tile;

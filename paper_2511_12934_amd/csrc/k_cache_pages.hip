@@ -117,21 +117,28 @@ template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_app
 // The way back: rows of a page to keys and vals (null: not wanted), which are written.  A thread takes 16 bytes of them, so that neighbours'
 // pieces make whole lines (16 histories of 20,011 rows, two heads of 128 in fp32: 145 us, in pieces
 // of 32 bytes 378).
-template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_read(ARGS list, CacheShape c)
+template <int DT> __global__ __launch_bounds__(256) void k_cache_read(CacheFew few /* first: kernel_arg */, const char *dev, int n_outs, CacheShape c)
 {
     constexpr int WIDE = DT == 0 ? 4 : 8, ESZ = DT == 0 ? 4 : 2;
-    const CacheUnit u = cache_desc<CacheUnit>(list, (size_t)blockIdx.x * sizeof(CacheUnit));
+    (void)few;
+    const int firsts = n_outs * (int)sizeof(CacheOut), out = entry_of(dev, n_outs, firsts, blockIdx.x, threadIdx.x & 63);
+    const CacheOut u = desc_at<CacheOut>(dev, out);
+    const int pieces = (c.page_len + UNIT_ROWS - 1) / UNIT_ROWS, unit = unit_of_row(u.first, c.page_len) + (int)blockIdx.x - first_at(dev, firsts, out);
+    const int in_seq = unit / pieces, from_row = unit % pieces * UNIT_ROWS, page_row = in_seq * c.page_len;
+    const int lo = max(page_row + from_row, u.first), n = min(page_row + min(from_row + UNIT_ROWS, c.page_len), u.first + u.n) - lo;
     const int head = blockIdx.y, dp = c.dp, per_row = dp / WIDE;
-    char *page = as_global(c.pool) + (size_t)u.page * c.page_bytes + (size_t)head * cache_head_bytes(c);
+    char *page = as_global(c.pool) + (size_t)as_global(c.table)[u.entry + in_seq] * c.page_bytes + (size_t)head * cache_head_bytes(c);
     const int step = 256 / per_row, at = threadIdx.x % per_row * WIDE;
-    char *keys = const_cast<char *>(as_global(u.keys)), *vals = const_cast<char *>(as_global(u.vals));
+    const size_t to = (size_t)head * c.d_head + at;
+    char *keys = u.keys ? as_global(u.keys) + ((size_t)(lo - u.first) * u.key_stride + to) * ESZ : nullptr;
+    char *vals = u.vals ? as_global(u.vals) + ((size_t)(lo - u.first) * u.val_stride + to) * ESZ : nullptr;
     if (at >= c.d_head) return;
-    for (int row = threadIdx.x / per_row; row < u.n && threadIdx.x < step * per_row; row += 4 * step) {
+    for (int row = threadIdx.x / per_row; row < n && threadIdx.x < step * per_row; row += 4 * step) {
         uint32_t codes[8], byte[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int r = row + i / 2 * step;
-            const RowAt from = row_at(page, dp, u.row0 + (r < u.n ? r : row));
+            const RowAt from = row_at(page, dp, lo - page_row + (r < n ? r : row));
             const char *p = from.codes + (i & 1 ? 16 * dp : 0) + at / 2;
             codes[i] = DT == 0 ? *(const uint16_t *)p : *(const uint32_t *)p;
             byte[i] = (uint8_t)from.scales[(i & 1 ? dp : 0) + at / CACHE_BLOCK];
@@ -140,7 +147,7 @@ template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_rea
         for (int i = 0; i < 8; ++i) {
             const int r = row + i / 2 * step;
             char *dst = i & 1 ? vals : keys;
-            if (r >= u.n || !dst) continue;
+            if (r >= n || !dst) continue;
             const float scale = __uint_as_float(byte[i] << 23);
             u32x4 v;
             v.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 0));
@@ -151,7 +158,7 @@ template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_rea
                 v.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 2));
                 v.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes[i], scale, 3));
             }
-            __builtin_nontemporal_store(v, (u32x4 *)(dst + ((size_t)r * (i & 1 ? u.val_stride : u.key_stride) + (size_t)head * c.d_head + at) * ESZ));
+            __builtin_nontemporal_store(v, (u32x4 *)(dst + (size_t)r * (i & 1 ? u.val_stride : u.key_stride) * ESZ));
         }
     }
 }
@@ -165,14 +172,12 @@ template <class ARGS> __global__ __launch_bounds__(256) void k_cache_fill(ARGS l
 
 constexpr int MOVE_PIECES = 4 * 256;            // at most, of one block: four pieces of 16 bytes a thread in flight
 
-template <class ARGS> __global__ __launch_bounds__(256) void k_cache_move(ARGS list, CacheShape c)
+// a page's blocks share it evenly
+__device__ __forceinline__ void move_page(const CacheShape &c, int from, int to)
 {
-    const CacheMove m = cache_desc<CacheMove>(list, (size_t)blockIdx.x * sizeof(CacheMove));
-    if (m.entry >= 0 && blockIdx.y == 0 && threadIdx.x == 0) c.table[m.entry] = m.dst;
-    if (m.src < 0) return;
-    const u32x4 *src = (const u32x4 *)(as_global(c.pool) + (size_t)m.src * c.page_bytes);
-    u32x4 *dst = (u32x4 *)(as_global(c.pool) + (size_t)m.dst * c.page_bytes);
-    const int all = (int)(c.page_bytes / 16), each = (all + gridDim.y - 1) / gridDim.y;         // a page's blocks share it evenly
+    const u32x4 *src = (const u32x4 *)(as_global(c.pool) + (size_t)from * c.page_bytes);
+    u32x4 *dst = (u32x4 *)(as_global(c.pool) + (size_t)to * c.page_bytes);
+    const int all = (int)(c.page_bytes / 16), each = (all + gridDim.y - 1) / gridDim.y;
     const int at = blockIdx.y * each + threadIdx.x, end = min(all, (int)(blockIdx.y + 1) * each);
     u32x4 v[4];
 #pragma unroll
@@ -181,6 +186,23 @@ template <class ARGS> __global__ __launch_bounds__(256) void k_cache_move(ARGS l
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (at + 256 * j < end) __builtin_nontemporal_store(v[j], dst + at + 256 * j);
+}
+template <class ARGS> __global__ __launch_bounds__(256) void k_cache_move(ARGS list, CacheShape c)
+{
+    const CacheMove m = cache_desc<CacheMove>(list, (size_t)blockIdx.x * sizeof(CacheMove));
+    if (m.entry >= 0 && blockIdx.y == 0 && threadIdx.x == 0) c.table[m.entry] = m.dst;
+    if (m.src >= 0) move_page(c, m.src, m.dst);
+}
+// Whole sequences: the pages that are copied are the table's to know, and the new ones mostly follow each other.  (A descriptor a page,
+// read from the host's memory: 14.8 us for 1,277 pages of 17 KB, 10 with runs of them in the arguments.)
+__global__ __launch_bounds__(256) void k_cache_copy(CacheFew few /* first: kernel_arg */, const char *dev, int n_runs, CacheShape c)
+{
+    (void)few;
+    const int firsts = n_runs * (int)sizeof(CacheRun), run = entry_of(dev, n_runs, firsts, blockIdx.x, threadIdx.x & 63);
+    const CacheRun m = desc_at<CacheRun>(dev, run);
+    const int i = (int)blockIdx.x - first_at(dev, firsts, run);
+    if (blockIdx.y == 0 && threadIdx.x == 0) c.table[m.dst + i] = m.page < 0 ? -1 : m.page + i;
+    if (m.page >= 0) move_page(c, as_global(c.table)[m.src + i], m.page + i);
 }
 
 }  // namespace
@@ -196,15 +218,26 @@ hipError_t launch_cache_append(const CacheShape &c, const CacheList &units, hipS
     });
 }
 
-hipError_t launch_cache_read(const CacheShape &c, const CacheList &units, hipStream_t s)
+hipError_t launch_cache_read(const CacheShape &c, const CacheList &outs, int units, hipStream_t s)
 {
-    if (units.n == 0) return hipSuccess;
-    return cache_launch(units, [&](auto args) {
-        using A = decltype(args);
-        const dim3 grid(units.n, c.n_kv);
-        if (c.dtype == 0) hipLaunchKernelGGL((k_cache_read<0, A>), grid, dim3(256), 0, s, args, c);
-        else hipLaunchKernelGGL((k_cache_read<1, A>), grid, dim3(256), 0, s, args, c);
-    });
+    if (units == 0) return hipSuccess;
+    CacheFew args;
+    if (!outs.dev) __builtin_memcpy(args.w, outs.host, outs.bytes);
+    const dim3 grid(units, c.n_kv);
+    if (c.dtype == 0) hipLaunchKernelGGL(k_cache_read<0>, grid, dim3(256), 0, s, args, outs.dev, outs.n, c);
+    else hipLaunchKernelGGL(k_cache_read<1>, grid, dim3(256), 0, s, args, outs.dev, outs.n, c);
+    return hipGetLastError();
+}
+
+static unsigned blocks_of_page(const CacheShape &c) { return (unsigned)((c.page_bytes / 16 + MOVE_PIECES - 1) / MOVE_PIECES); }
+
+hipError_t launch_cache_copy(const CacheShape &c, const CacheList &runs, int pages, hipStream_t s)
+{
+    if (pages == 0) return hipSuccess;
+    CacheFew args;
+    if (!runs.dev) __builtin_memcpy(args.w, runs.host, runs.bytes);
+    hipLaunchKernelGGL(k_cache_copy, dim3(pages, blocks_of_page(c)), dim3(256), 0, s, args, runs.dev, runs.n, c);
+    return hipGetLastError();
 }
 
 hipError_t launch_cache_fill(const CacheShape &c, const CacheList &fills, int longest, hipStream_t s)
@@ -219,7 +252,7 @@ hipError_t launch_cache_move(const CacheShape &c, const CacheList &moves, hipStr
 {
     if (moves.n == 0) return hipSuccess;
     return cache_launch(moves, [&](auto args) {
-        hipLaunchKernelGGL((k_cache_move<decltype(args)>), dim3(moves.n, (unsigned)((c.page_bytes / 16 + MOVE_PIECES - 1) / MOVE_PIECES)), dim3(256), 0, s, args, c);
+        hipLaunchKernelGGL((k_cache_move<decltype(args)>), dim3(moves.n, blocks_of_page(c)), dim3(256), 0, s, args, c);
     });
 }
 

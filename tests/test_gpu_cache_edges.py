@@ -134,3 +134,32 @@ def test_entries_alike_and_not_give_the_same_bits(torch, n, n_q, longest, window
     for u in (0, n // 2, n - 1):
         k = held[longest - lens[u]:]
         compare("bf16", got[0][0][u][some], got[0][1][u][some], q_host[u][some], k, k, d ** -0.5, positions=where[u][some] if window else None, sinks=3, window=window, what=f"entry {u}")
+
+
+@pytest.mark.parametrize("dtype,kv,d,pl", [("bf16", 2, 64, 32), ("f32", 1, 40, 96)])
+def test_copies_into_a_pool_of_scattered_pages(torch, dtype, kv, d, pl):
+    """More runs of pages than a launch's arguments hold, dropped pages among them, rows read from the middle of pages."""
+    _say(f"scattered copies {dtype} page={pl}")
+    rng = np.random.default_rng(pl)
+    n_pages = 220
+    longest = n_pages * pl
+    ctx = make(torch, dtype, kv, kv, d, pl, pages=3 * n_pages, seqs=5, longest=longest, requests=2)
+    k, v = rows(rng, longest - 5, kv, d, dtype), rows(rng, longest - 5, kv, d, dtype)
+    dk, dv = dev(torch, k, dtype), dev(torch, v, dtype)
+    for lo in range(0, longest - 5, pl):
+        ctx.aif_cache_append([B.CacheAppend(u, dk[lo:lo + pl], dv[lo:lo + pl]) for u in (0, 1)])
+    ctx.aif_cache_fork([0], [2])
+    ctx.aif_cache_trim([2], sinks=10, window=longest - 9 * pl)
+    ctx.aif_cache_free([1])
+    ctx.aif_cache_copy([0, 2], [3, 4])
+    hk, hv = ref.hold(k), ref.hold(v)
+    for first, n in ((0, longest - 5), (pl - 1, 2), (7, 1), (5 * pl + 3, 3 * pl), (longest - 6, 1), (longest - 5, 0)):
+        gk, gv = read(torch, ctx, dtype, 3, kv, d, first=first, n=n)
+        assert np.array_equal(gk, hk[first:first + n]) and np.array_equal(gv, hv[first:first + n]), (first, n)
+    gk, _ = read(torch, ctx, dtype, 4, kv, d, first=10 * pl, n=4 * pl)
+    assert np.array_equal(gk, hk[10 * pl:14 * pl])
+    with pytest.raises(B.AifError, match="dropped"):
+        read(torch, ctx, dtype, 4, kv, d, first=2 * pl, n=1)
+    q = wl.round_storage(rng.standard_normal((2, kv, d)).astype(np.float32), dtype)
+    gone = ((pl, (longest - 5 - (longest - 9 * pl)) // pl * pl),)
+    check_attend(torch, ctx, dtype, 4, k, v, q, scale=d ** -0.5, dropped=gone, what="a copy with dropped pages")
