@@ -5,7 +5,7 @@
 // buffers.  Products are 32x32x16: S^T = K Q^T with a wave's queries in registers throughout, so that a lane holds 16 keys
 // of one row, and these, as weights, are the operand of O^T = V^T P^T as they stand; V comes turned (ds_read_b64_tr_b16).  What bounds it is
 // the vector ALU: per score one fused multiply-add, half a maximum, one exponential (2.3 times a plain instruction), half a conversion and one
-// addition.  Heads of 64: eight waves of 32 rows, four waves a SIMD (64 x 10^4 rows over 500 keys 125 us, 0.65
+// addition.  Heads of 64: eight waves of 32 rows, four waves a SIMD (64 x 10^4 rows over 500 keys 121 us, 0.68
 // PFLOP/s; four waves of 64 rows that each bring the keys over for themselves, k_cache_own.hip, 130).
 // Rows of K are 16 bytes longer than their features: the lanes of a read meet different banks (V: v_place).
 #include "k_cache_attend.h"

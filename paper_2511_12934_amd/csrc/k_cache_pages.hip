@@ -115,7 +115,7 @@ template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_app
 }
 
 // The way back: rows of a page to keys and vals (null: not wanted), which are written.  A thread takes 16 bytes of them, so that neighbours'
-// pieces make whole lines (16 histories of 20,011 rows, two heads of 128 in fp32: 145 us, in pieces
+// pieces make whole lines (16 histories of 20,011 rows, two heads of 128 in fp32: 142 us, in pieces
 // of 32 bytes 378).
 template <int DT> __global__ __launch_bounds__(256) void k_cache_read(CacheFew few /* first: kernel_arg */, const char *dev, int n_outs, CacheShape c)
 {
