@@ -71,7 +71,7 @@ typedef struct {
 } aif_cache_config;
 
 /* Rows for the end of a sequence.  keys and vals: DEVICE, 16-byte aligned, row i at i * stride elements, strides multiples
- * of 16 bytes (0: rows lie close, stride = n_kv_heads * d_head); vals may alias keys. */
+ * of 16 bytes below 2^33 elements (0: rows lie close, stride = n_kv_heads * d_head); vals may alias keys. */
 typedef struct {
     int32_t seq;
     int32_t n_rows;         /* >= 0 */

@@ -123,7 +123,7 @@ aif_status check_tensor(aif_cache_ctx *c, const char *what, int i, const void *p
     const int vec = c->shape.dtype == 0 ? 4 : 8;
     if (!p) return cfail(c, AIF_EINVAL, "%s %d: NULL tensor pointer", what, i);
     if ((uintptr_t)p % 16 || stride % vec) return cfail(c, AIF_EINVAL, "%s %d: tensors and strides must be multiples of 16 bytes", what, i);
-    if (stride != 0 && (stride < width || stride > (int64_t)1 << 40)) return cfail(c, AIF_EINVAL, "%s %d: stride %lld below the row's %d", what, i, (long long)stride, width);
+    if (stride != 0 && (stride < width || stride >= (int64_t)1 << 33)) return cfail(c, AIF_EINVAL, "%s %d: stride %lld below the row's %d, or 2^33 and above", what, i, (long long)stride, width);
     return AIF_OK;
 }
 
@@ -224,6 +224,47 @@ template <class F> aif_status send_list(aif_cache_ctx *c, const char *h, int n, 
     CACHE_TRY(c, go(l));
     return AIF_OK;
 }
+
+// Rows that are appended, as runs of rows on pages that follow each other.
+class CacheIns {
+public:
+    CacheIns(aif_cache_ctx *c, hipStream_t s) : c_(c), s_(s), ins_((CacheIn *)c->list.data()) {}
+    aif_status add(const CacheIn &in)
+    {
+        if (n_ == ROOM || rows_ >= MOST) {
+            const aif_status st = send();
+            if (st != AIF_OK) return st;
+        }
+        ins_[n_++] = in;
+        rows_ += in.n;
+        return AIF_OK;
+    }
+    // whether the last run may become longer, and further rows for it
+    bool open() const { return n_ && rows_ < MOST; }
+    void more(int32_t rows) { ins_[n_ - 1].n += rows, rows_ += rows; }
+    aif_status send()
+    {
+        if (n_ == 0) return AIF_OK;
+        int32_t *first = (int32_t *)(ins_ + n_), units = 0;
+        const int n = n_, pl = c_->cfg.page_len;
+        for (int i = 0; i < n; ++i) {
+            first[i] = units;
+            units += unit_of_row(ins_[i].have + ins_[i].n - 1, pl) - unit_of_row(ins_[i].have, pl) + 1;
+        }
+        first[n] = units;
+        n_ = rows_ = 0;
+        return send_list(c_, (const char *)ins_, n, n * sizeof(CacheIn) + (n + 1) * sizeof(int32_t), s_,
+                         [&](const CacheList &l) { return launch_cache_append(c_->shape, l, units, s_); });
+    }
+
+private:
+    static constexpr int ROOM = CACHE_LIST_BYTES / (sizeof(CacheIn) + sizeof(int32_t)) - 1;
+    static constexpr int MOST = 1 << 27;    // rows of a launch, about: units of 32 at least
+    aif_cache_ctx *c_;
+    hipStream_t s_;
+    CacheIn *ins_;
+    int n_ = 0, rows_ = 0;
+};
 
 // Pages that are copied, as runs of new ones that follow each other.
 class CacheCopies {
@@ -366,16 +407,13 @@ int32_t aif_cache_len(const aif_cache_ctx *ctx, int32_t seq) { return !ctx || se
 
 int32_t aif_cache_free_pages(const aif_cache_ctx *ctx) { return ctx ? ctx->book.n_free : -1; }
 
-// about the runs that n rows are cut into
-static int64_t runs_of(int64_t n, int page_len) { return n == 0 ? 0 : 1 + n / UNIT_ROWS + n / page_len; }
-
 aif_status aif_cache_append(aif_cache_ctx *c, const aif_cache_append_req *reqs, int32_t n, void *hip_stream)
 {
     if (!c) return AIF_EINVAL;
     aif_status st = check_count(c, reqs, n, c->cfg.max_requests);
     if (st != AIF_OK) return st;
     const int width = c->shape.n_kv * c->shape.d_head, pl = c->cfg.page_len;
-    int64_t pages = 0, units = 0;
+    int64_t pages = 0;
     name_none(c);
     for (int r = 0; r < n; ++r) {
         const aif_cache_append_req &q = reqs[r];
@@ -388,25 +426,28 @@ aif_status aif_cache_append(aif_cache_ctx *c, const aif_cache_append_req *reqs, 
         const int len = c->book.len(q.seq);
         if (q.n_rows > c->cfg.max_len - len) return cfail(c, AIF_ERANGE, "append %d: %d rows behind %d exceed max_len %d", r, q.n_rows, len, c->cfg.max_len);
         pages += c->book.append_needs(q.seq, q.n_rows);
-        units += runs_of(q.n_rows, pl);
     }
     if (pages > c->book.n_free) return cfail(c, AIF_ERANGE, "%lld pages needed, %d are free", (long long)pages, c->book.n_free);
     hipStream_t s = (hipStream_t)hip_stream;
     if ((st = check_stream(c, s)) != AIF_OK) return st;
 
-    CacheBatch<CacheUnit> batch(c, (size_t)units, s);
-    auto go = [&](const CacheList &l) { return launch_cache_append(c->shape, l, s); };
-    const int esz = c->shape.dtype == 0 ? 4 : 2;
+    const int64_t esz = c->shape.dtype == 0 ? 4 : 2;
+    CacheIns ins(c, s);
     for (int r = 0; r < n && st == AIF_OK; ++r) {
         const aif_cache_append_req &q = reqs[r];
-        const int64_t ks = q.key_stride ? q.key_stride : width, vs = q.val_stride ? q.val_stride : width;
-        c->book.append(q.seq, q.n_rows, UNIT_ROWS, [&](int32_t done, int32_t i, int32_t cow, int32_t row0, int32_t rows) {
-            const CacheUnit u{(const char *)q.keys + done * ks * esz, (const char *)q.vals + done * vs * esz, ks, vs, c->book.page(q.seq, i), cow,
-                              row0, rows, c->book.entry(q.seq, i), 0};
-            if (st == AIF_OK) st = batch.add(u, go);
+        const int64_t ks = (q.key_stride ? q.key_stride : width) * esz, vs = (q.val_stride ? q.val_stride : width) * esz;
+        const int have = c->book.len(q.seq);
+        int32_t next = -1;              // the page that would go on with the last run
+        c->book.append(q.seq, q.n_rows, pl, [&](int32_t done, int32_t i, int32_t cow, int32_t, int32_t rows) {
+            const int32_t page = c->book.page(q.seq, i);
+            if (st != AIF_OK) return;
+            if (page == next && ins.open()) ins.more(rows);
+            else st = ins.add(CacheIn{(const char *)q.keys + done * ks, (const char *)q.vals + done * vs, (uint32_t)(ks / 16), (uint32_t)(vs / 16), c->book.entry(q.seq, 0),
+                                      have + done, rows, page, cow, 0});
+            next = page + 1;
         });
     }
-    if (st == AIF_OK) st = batch.send(go);
+    if (st == AIF_OK) st = ins.send();
     c->book.settle();
     return st;
 }

@@ -27,13 +27,13 @@ struct CacheShape {
 __host__ __device__ inline size_t cache_tile_bytes(int dp) { return (size_t)34 * dp; }
 __host__ __device__ inline size_t cache_head_bytes(const CacheShape &c) { return (size_t)(c.page_len / CACHE_TILE) * 34 * c.dp; }
 
-// Rows [row0, row0 + n) of one page, from keys and vals on (strides in elements).
-struct CacheUnit {
+// n rows for the end of a sequence of `have` rows whose table entries start at `entry`, to the pages from `page` on, which follow each other; the first
+// row goes into the first of them.  cow >= 0: that page is a new one in the place of page cow, whose rows before `have` it gets first.
+struct CacheIn {
     const char *keys, *vals;
-    int64_t key_stride, val_stride;
-    int32_t page, cow;          // cow >= 0: the page's rows before row0 come from that page first
-    int32_t row0, n;
-    int32_t entry, pad_;        // the table entry that names the page
+    uint32_t key_stride, val_stride;    // in 16 bytes
+    int32_t entry, have, n;
+    int32_t page, cow, pad_;
 };
 // Rows [first, first + n) of a sequence whose table entries start at `entry`, to keys and vals (or null; strides in elements).
 struct CacheOut {
@@ -94,8 +94,8 @@ struct CacheList {
 };
 inline size_t cache_asks_bytes(int n, bool lean) { return lean ? sizeof(CacheLean) + n * sizeof(CacheOwn) : n * sizeof(CacheAsk); }
 
-hipError_t launch_cache_append(const CacheShape &c, const CacheList &units, hipStream_t s);
-// outs: n CacheOut, then int32 first[n + 1], running numbers of their units (see unit_of_row); runs: n CacheRun, then those of their pages.
+// ins: n CacheIn, then int32 first[n + 1], running numbers of their units (see unit_of_row); outs likewise; runs: n CacheRun, then those of their pages.
+hipError_t launch_cache_append(const CacheShape &c, const CacheList &ins, int units, hipStream_t s);
 hipError_t launch_cache_read(const CacheShape &c, const CacheList &outs, int units, hipStream_t s);
 hipError_t launch_cache_copy(const CacheShape &c, const CacheList &runs, int pages, hipStream_t s);
 hipError_t launch_cache_fill(const CacheShape &c, const CacheList &fills, int longest, hipStream_t s);
@@ -134,19 +134,19 @@ __device__ __forceinline__ int first_at(const char *dev, int firsts, int i)
     const size_t off = (size_t)firsts + 4 * (size_t)i;
     return dev ? *(const int32_t *)(as_global(dev) + off) : *kernel_arg<int32_t>(off);
 }
-// The entry that a unit belongs to, by running numbers int32 first[n + 1] at byte `firsts` of the descriptors: 64 of them at a time.
+// The entry that a unit belongs to, by running numbers int32 first[n + 1] at byte `firsts` of the descriptors: 64 of them are looked at at a time.
 __device__ __forceinline__ int entry_of(const char *dev, int n, int firsts, int unit, int lane)
 {
-    int r = 0;
-    for (int base = 1; base <= n; base += 64) {
-        const int i = base + lane;
-        const int f = first_at(dev, firsts, i <= n ? i : n);
-        const int below = __popcll(__ballot(i <= n && f <= unit));
-        r += below;
-        if (below < 64) break;
+    int r = 0, end = n;                 // first[r] <= unit < first[end + 1]
+    while (r < end) {
+        const int step = (end - r + 63) / 64, i = r + (lane + 1) * step;
+        const int f = first_at(dev, firsts, i <= end ? i : end);
+        r += step * __builtin_amdgcn_readfirstlane(__popcll(__ballot(i <= end && f <= unit)));
+        end = min(end, r + step - 1);
     }
-    return __builtin_amdgcn_readfirstlane(r);
+    return r;
 }
+
 template <class F> hipError_t cache_launch(const CacheList &list, F &&go)
 {
     if (list.dev) {

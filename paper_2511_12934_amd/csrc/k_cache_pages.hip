@@ -68,24 +68,45 @@ __device__ __forceinline__ RowAt row_at(char *head, int dp, int row)
     return RowAt{tile + r * (dp / 2), tile + 32 * dp + r * (dp / 32)};
 }
 
-// One block: one unit, one head.  It names the page in the table, brings the rows that a shared page held, and writes its own.
-template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_append(ARGS list, CacheShape c)
+// Of n rows of a sequence from `first` on, those in the unit-th unit that they touch: rows [lo, lo + n) on page in_seq, which begins with row page_row.
+struct UnitRows {
+    int in_seq, page_row, lo, n;
+};
+__device__ __forceinline__ UnitRows unit_rows(int first, int n, int unit, int page_len)
 {
-    const CacheUnit u = cache_desc<CacheUnit>(list, (size_t)blockIdx.x * sizeof(CacheUnit));
+    const int pieces = (page_len + UNIT_ROWS - 1) / UNIT_ROWS;
+    unit += unit_of_row(first, page_len);
+    UnitRows u;
+    u.in_seq = unit / pieces;
+    u.page_row = u.in_seq * page_len;
+    const int from = unit % pieces * UNIT_ROWS;
+    u.lo = max(u.page_row + from, first);
+    u.n = min(u.page_row + min(from + UNIT_ROWS, page_len), first + n) - u.lo;
+    return u;
+}
+
+// One block: rows of one page, one head.  It names the page in the table, brings the rows that a shared page held, and writes its own.
+template <int DT> __global__ __launch_bounds__(256) void k_cache_append(CacheFew few /* first: kernel_arg */, const char *dev, int n_ins, CacheShape c)
+{
+    (void)few;
+    const int firsts = n_ins * (int)sizeof(CacheIn), in = entry_of(dev, n_ins, firsts, blockIdx.x, threadIdx.x & 63);
+    const CacheIn u = desc_at<CacheIn>(dev, in);
+    const UnitRows at_rows = unit_rows(u.have, u.n, (int)blockIdx.x - first_at(dev, firsts, in), c.page_len);
+    const int row0 = at_rows.lo - at_rows.page_row, page_no = u.page + at_rows.in_seq - u.have / c.page_len;
     const int head = blockIdx.y, dp = c.dp, per_row = dp / 8, esz = DT == 0 ? 4 : 2;
-    char *page = as_global(c.pool) + (size_t)u.page * c.page_bytes + (size_t)head * cache_head_bytes(c);
-    if (threadIdx.x == 0 && head == 0) c.table[u.entry] = u.page;
-    if (u.cow >= 0) {
+    char *page = as_global(c.pool) + (size_t)page_no * c.page_bytes + (size_t)head * cache_head_bytes(c);
+    if (threadIdx.x == 0 && head == 0) c.table[u.entry + at_rows.in_seq] = page_no;
+    if (u.cow >= 0 && at_rows.lo == u.have) {
         const char *from = c.pool + (size_t)u.cow * c.page_bytes + (size_t)head * cache_head_bytes(c);
         // codes in pieces of 16 bytes, scales byte by byte: the rest of either belongs to rows that this launch writes
         const int pieces = dp / 32, nb = dp / 32;
-        for (int i = threadIdx.x; i < u.row0 * pieces; i += 256) {
+        for (int i = threadIdx.x; i < row0 * pieces; i += 256) {
             const int row = i / pieces, at = i % pieces * 16;
             const RowAt a = row_at((char *)from, dp, row), b = row_at(page, dp, row);
             *(uint4 *)(b.codes + at) = *(const uint4 *)(a.codes + at);
             *(uint4 *)(b.codes + 16 * dp + at) = *(const uint4 *)(a.codes + 16 * dp + at);
         }
-        for (int i = threadIdx.x; i < u.row0 * nb; i += 256) {
+        for (int i = threadIdx.x; i < row0 * nb; i += 256) {
             const int row = i / nb, at = i % nb;
             const RowAt a = row_at((char *)from, dp, row), b = row_at(page, dp, row);
             b.scales[at] = a.scales[at];
@@ -94,20 +115,21 @@ template <int DT, class ARGS> __global__ __launch_bounds__(256) void k_cache_app
     }
     // a thread keeps its features; two rows' keys and values are asked for before the first is worked on
     const int step = 256 / per_row, at = threadIdx.x % per_row * 8;
-    const char *keys = as_global(u.keys) + (size_t)head * c.d_head * esz, *vals = as_global(u.vals) + (size_t)head * c.d_head * esz;
-    for (int row = threadIdx.x / per_row; row < u.n && threadIdx.x < step * per_row; row += 2 * step) {
+    const size_t ks = (size_t)u.key_stride * 16, vs = (size_t)u.val_stride * 16, done = at_rows.lo - u.have;
+    const char *keys = as_global(u.keys) + done * ks + (size_t)head * c.d_head * esz, *vals = as_global(u.vals) + done * vs + (size_t)head * c.d_head * esz;
+    for (int row = threadIdx.x / per_row; row < at_rows.n && threadIdx.x < step * per_row; row += 2 * step) {
         float x[4][8];
-        const bool two = row + step < u.n;
-        load8<DT>(keys + (size_t)row * u.key_stride * esz, at, c.d_head, x[0]);
-        load8<DT>(vals + (size_t)row * u.val_stride * esz, at, c.d_head, x[1]);
-        load8<DT>(keys + (size_t)(two ? row + step : row) * u.key_stride * esz, at, c.d_head, x[2]);
-        load8<DT>(vals + (size_t)(two ? row + step : row) * u.val_stride * esz, at, c.d_head, x[3]);
+        const bool two = row + step < at_rows.n;
+        load8<DT>(keys + row * ks, at, c.d_head, x[0]);
+        load8<DT>(vals + row * vs, at, c.d_head, x[1]);
+        load8<DT>(keys + (two ? row + step : row) * ks, at, c.d_head, x[2]);
+        load8<DT>(vals + (two ? row + step : row) * vs, at, c.d_head, x[3]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (i >= 2 && !two) break;
             uint32_t byte;
             const uint32_t codes = encode8(x[i], byte);
-            const RowAt to = row_at(page, dp, u.row0 + row + (i >= 2 ? step : 0));
+            const RowAt to = row_at(page, dp, row0 + row + (i >= 2 ? step : 0));
             *(uint32_t *)(to.codes + (i & 1 ? 16 * dp : 0) + at / 2) = codes;
             if (at % CACHE_BLOCK == 0) to.scales[(i & 1 ? dp : 0) + at / CACHE_BLOCK] = (char)byte;
         }
@@ -123,11 +145,10 @@ template <int DT> __global__ __launch_bounds__(256) void k_cache_read(CacheFew f
     (void)few;
     const int firsts = n_outs * (int)sizeof(CacheOut), out = entry_of(dev, n_outs, firsts, blockIdx.x, threadIdx.x & 63);
     const CacheOut u = desc_at<CacheOut>(dev, out);
-    const int pieces = (c.page_len + UNIT_ROWS - 1) / UNIT_ROWS, unit = unit_of_row(u.first, c.page_len) + (int)blockIdx.x - first_at(dev, firsts, out);
-    const int in_seq = unit / pieces, from_row = unit % pieces * UNIT_ROWS, page_row = in_seq * c.page_len;
-    const int lo = max(page_row + from_row, u.first), n = min(page_row + min(from_row + UNIT_ROWS, c.page_len), u.first + u.n) - lo;
+    const UnitRows at_rows = unit_rows(u.first, u.n, (int)blockIdx.x - first_at(dev, firsts, out), c.page_len);
+    const int lo = at_rows.lo, n = at_rows.n, page_row = at_rows.page_row;
     const int head = blockIdx.y, dp = c.dp, per_row = dp / WIDE;
-    char *page = as_global(c.pool) + (size_t)as_global(c.table)[u.entry + in_seq] * c.page_bytes + (size_t)head * cache_head_bytes(c);
+    char *page = as_global(c.pool) + (size_t)as_global(c.table)[u.entry + at_rows.in_seq] * c.page_bytes + (size_t)head * cache_head_bytes(c);
     const int step = 256 / per_row, at = threadIdx.x % per_row * WIDE;
     const size_t to = (size_t)head * c.d_head + at;
     char *keys = u.keys ? as_global(u.keys) + ((size_t)(lo - u.first) * u.key_stride + to) * ESZ : nullptr;
@@ -207,15 +228,15 @@ __global__ __launch_bounds__(256) void k_cache_copy(CacheFew few /* first: kerne
 
 }  // namespace
 
-hipError_t launch_cache_append(const CacheShape &c, const CacheList &units, hipStream_t s)
+hipError_t launch_cache_append(const CacheShape &c, const CacheList &ins, int units, hipStream_t s)
 {
-    if (units.n == 0) return hipSuccess;
-    return cache_launch(units, [&](auto args) {
-        using A = decltype(args);
-        const dim3 grid(units.n, c.n_kv);
-        if (c.dtype == 0) hipLaunchKernelGGL((k_cache_append<0, A>), grid, dim3(256), 0, s, args, c);
-        else hipLaunchKernelGGL((k_cache_append<1, A>), grid, dim3(256), 0, s, args, c);
-    });
+    if (units == 0) return hipSuccess;
+    CacheFew args;
+    if (!ins.dev) __builtin_memcpy(args.w, ins.host, ins.bytes);
+    const dim3 grid(units, c.n_kv);
+    if (c.dtype == 0) hipLaunchKernelGGL(k_cache_append<0>, grid, dim3(256), 0, s, args, ins.dev, ins.n, c);
+    else hipLaunchKernelGGL(k_cache_append<1>, grid, dim3(256), 0, s, args, ins.dev, ins.n, c);
+    return hipGetLastError();
 }
 
 hipError_t launch_cache_read(const CacheShape &c, const CacheList &outs, int units, hipStream_t s)

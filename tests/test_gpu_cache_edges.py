@@ -163,3 +163,53 @@ def test_copies_into_a_pool_of_scattered_pages(torch, dtype, kv, d, pl):
     q = wl.round_storage(rng.standard_normal((2, kv, d)).astype(np.float32), dtype)
     gone = ((pl, (longest - 5 - (longest - 9 * pl)) // pl * pl),)
     check_attend(torch, ctx, dtype, 4, k, v, q, scale=d ** -0.5, dropped=gone, what="a copy with dropped pages")
+
+
+def test_a_history_onto_scattered_pages(torch):
+    """Rows appended to more runs of pages than a launch's arguments hold, the first of them a shared page."""
+    _say("an append onto scattered pages")
+    rng = np.random.default_rng(8)
+    pl, d, n_pages = 32, 32, 300
+    ctx = make(torch, "bf16", 1, 1, d, pl, pages=n_pages, seqs=n_pages + 2, longest=n_pages * pl, requests=n_pages)
+    some = rows(rng, n_pages * pl, 1, d, "bf16")
+    t = dev(torch, some, "bf16")
+    ctx.aif_cache_append([B.CacheAppend(u, t[u:u + 20], t[u:u + 20]) for u in range(n_pages)])
+    ctx.aif_cache_free(list(range(0, n_pages, 2)))
+    ctx.aif_cache_fork([1, 1], [n_pages, n_pages + 1])
+    more = 140 * pl
+    ctx.aif_cache_append([B.CacheAppend(n_pages, t[:more], t[:more]), B.CacheAppend(n_pages + 1, t[5:9], t[5:9])])
+    want = np.concatenate([some[1:21], some[:more]])
+    assert np.array_equal(read(torch, ctx, "bf16", n_pages, 1, d)[0], ref.hold(want))
+    assert np.array_equal(read(torch, ctx, "bf16", n_pages + 1, 1, d)[1], ref.hold(np.concatenate([some[1:21], some[5:9]])))
+    for u in (1, 3, 151, n_pages - 1):
+        assert np.array_equal(read(torch, ctx, "bf16", u, 1, d)[0], ref.hold(some[u:u + 20])), u
+
+
+@pytest.mark.parametrize("dtype,n", [("bf16", 70), ("f32", 700)])
+def test_many_unlike_entries_in_one_call(torch, dtype, n):
+    """More entries than a wave has lanes: appends, queries and reads of unlike lengths, some of none."""
+    _say(f"{n} unlike entries {dtype}")
+    rng = np.random.default_rng(n)
+    kv, heads, d, pl = 2, 4, 40, 64
+    ctx = make(torch, dtype, heads, kv, d, pl, pages=6 * n, seqs=n, longest=300, requests=n, queries=90)
+    lens, n_qs = rng.integers(0, 300, n), rng.integers(0, 3, n) * rng.integers(0, 45, n)
+    lens[::7], n_qs[5::9] = 0, 1
+    k, v = rows(rng, 400, kv, d, dtype), rows(rng, 400, kv, d, dtype)
+    dk, dv = dev(torch, k, dtype), dev(torch, v, dtype)
+    cuts = np.minimum(lens, rng.integers(0, 300, n))
+    ctx.aif_cache_append([B.CacheAppend(u, dk[u % 90:u % 90 + cuts[u]], dv[u % 90:u % 90 + cuts[u]]) for u in range(n)])
+    ctx.aif_cache_append([B.CacheAppend(u, dk[u % 90 + cuts[u]:u % 90 + lens[u]], dv[u % 90 + cuts[u]:u % 90 + lens[u]]) for u in rng.permutation(n)])
+    order = rng.permutation(n)
+    q_host = wl.round_storage(rng.standard_normal((90, heads, d)).astype(np.float32), dtype)
+    q = dev(torch, q_host, dtype)
+    outs = {u: torch.full_like(q[:n_qs[u]], float("nan")) for u in order}
+    lse = {u: torch.full((int(n_qs[u]), heads), float("nan"), device="cuda") for u in order}
+    ctx.aif_cache_attend([B.CacheQuery(int(u), q[:n_qs[u]], outs[u], lse=lse[u]) for u in order])
+    back = [torch.zeros((int(m), kv, d), device="cuda").to(dk.dtype) for m in lens]
+    ctx.aif_cache_read([B.CacheRead(int(u), None, back[u]) for u in order])
+    torch.cuda.synchronize()
+    for u in range(n):
+        assert np.array_equal(back[u].float().cpu().numpy(), ref.hold(v[u % 90:u % 90 + lens[u]])), u
+    for u in [int(x) for x in order if n_qs[x]][:25]:
+        at = slice(u % 90, u % 90 + int(lens[u]))
+        compare(dtype, outs[u].float().cpu().numpy(), lse[u].cpu().numpy(), q_host[:n_qs[u]], k[at], v[at], d ** -0.5, what=f"entry {u}")
