@@ -57,12 +57,9 @@ class Call:
             check()
 
 
-@pytest.mark.parametrize("dtype,heads,kv,d", WIDTHS)
-@pytest.mark.parametrize("whole", (20000, 140000))
+@pytest.mark.parametrize("dtype,heads,kv,d,whole", [(*w, 20000) for w in WIDTHS] + [(*w, 140000) for w in WIDTHS if w[0] == "bf16" and w[3] <= 128])
 def test_entries_beside_one_that_fills_the_device(torch, dtype, heads, kv, d, whole):
     """`whole`: rows of the entry that fills it, for row tiles of 128 and, where there are any, of 256."""
-    if whole > 20000 and (dtype == "f32" or d > 128):
-        pytest.skip("row tiles of 128 only")
     _say(f"beside {whole} rows: {dtype} heads={heads}/{kv} d={d}")
     rng = np.random.default_rng(d + whole)
     group = heads // kv
