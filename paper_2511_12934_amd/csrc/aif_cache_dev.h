@@ -112,6 +112,7 @@ struct CachePart {
     int32_t units, joins;       // of all asks
     int32_t each;               // > 0: every entry has that many units
     int32_t rows_of_tile;
+    bool eight;                 // few rows: blocks of eight waves, not four
     bool own;                   // many rows: the kernel whose waves bring keys and values to bf16 for themselves
     float *part;                // partial results of split keys, a unit and kv head each: [rows][dp] sums, [rows] maxima, [rows] sums of weights
 };

@@ -10,7 +10,7 @@
 // the 16x16x32 products: S^T = K Q^T (a lane's codes of a key are the k-slots; which features stand in which slot is free, so a
 // lane takes dp / 4 neighbouring ones), whose result leaves a lane with eight keys of ONE row: the weights are the second
 // product's operand where they are, O^T = V^T P^T.  V has to be turned, features to rows: bf16 rows of 32 keys in the wave's own LDS,
-// read back by ds_read_b64_tr_b16 (four keys of one feature a lane; v_place keeps the lanes to different banks).  No barrier in the loop; the four waves of a block take the tiles in turn, each
+// read back by ds_read_b64_tr_b16 (four keys of one feature a lane; v_place keeps the lanes to different banks).  No barrier in the loop; the four or eight waves of a block take the tiles in turn, each
 // with the next tile's codes already asked for, and join through LDS.  16 users' histories of 131,072 behaviours, 4 kv heads of 128, one query of 16 heads:
 // 201 us, 5.7 TB/s.  With 32 rows to a tile conversions, products and softmax take as long as the bytes do: 0.25 us a tile and block at heads of 128, the bytes
 // at that rate 0.20.  Short calls take the launch, 4 us of loads one behind the other (arguments, table, codes), and the
@@ -102,13 +102,13 @@ template <int DT> __device__ __forceinline__ void store_row(const CacheAsk &a, c
     else *(bf16x4 *)out = __builtin_convertvector(v, bf16x4);
 }
 
-template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache_few(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
+template <int DT, int NW, int NT, int WAVES> __global__ __launch_bounds__(64 * WAVES) void k_cache_few(CacheFew few /* first: kernel_arg */, const char *dev, CacheGrid g, CacheShape c, float *part)
 {
     constexpr int DP = 32 * NW, NP = DT == 0 ? 3 : 1, ROWS = 16 * NT, FT = DP / 16;
     constexpr int WAVE_BYTES = 64 * DP + 256;       // 32 rows of values; in the end 16 rows of sums, four apart
     static_assert(WAVE_BYTES == 16 * (DP + 4) * 4);
-    __shared__ __align__(16) char lds[4 * WAVE_BYTES];
-    __shared__ float ml[2][4][ROWS], total[2][ROWS];
+    __shared__ __align__(16) char lds[WAVES * WAVE_BYTES];
+    __shared__ float ml[2][WAVES][ROWS], total[2][ROWS];
     (void)few;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, grp = lane >> 4, kvh = blockIdx.y;
     const AskUnit found = block_ask(dev, g, lane);
@@ -150,10 +150,10 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     typedef s16x4 __attribute__((address_space(3))) *lds4_t;
 
     TileList<DP> list;
-    list.fill(c, a, walk, t, 4, t_end, lane);
+    list.fill(c, a, walk, t, WAVES, t_end, lane);
     auto ask = [&](int t, RawTile<NW> &to) {            // a tile that is dropped or behind the end reads page 0
-        if (t - list.from >= 256) list.fill(c, a, walk, t, 4, t_end, lane);
-        const int64_t off = list.offset((t - list.from) / 4);
+        if (t - list.from >= 64 * WAVES) list.fill(c, a, walk, t, WAVES, t_end, lane);
+        const int64_t off = list.offset((t - list.from) / WAVES);
         to.here = off >= 0;
         load_tile<NW>(pool + (off < 0 ? 0 : off), lane, to);
     };
@@ -260,7 +260,7 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     RawTile<NW> raw[DEPTH];
 #pragma unroll
     for (int i = 0; i < DEPTH - 1; ++i) {
-        ask(t + 4 * i, raw[i]);
+        ask(t + WAVES * i, raw[i]);
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
@@ -274,15 +274,15 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
             for (int j = 0; j < NP; ++j) q[i][j][w] = p[j];
         }
     }
-    for (; t < t_end; t += 4 * DEPTH)
+    for (; t < t_end; t += WAVES * DEPTH)
 #pragma unroll
         for (int i = 0; i < DEPTH; ++i) {
-            ask(t + 4 * (i + DEPTH - 1), raw[(i + DEPTH - 1) % DEPTH]);
+            ask(t + WAVES * (i + DEPTH - 1), raw[(i + DEPTH - 1) % DEPTH]);
             __builtin_amdgcn_sched_barrier(0);
-            work(t + 4 * i, raw[i]);
+            work(t + WAVES * i, raw[i]);
         }
 
-    // the four waves' parts become one: a common reference, then sums through LDS
+    // the waves' parts become one: a common reference, then sums through LDS
 #pragma unroll
     for (int i = 0; i < NT; ++i) {
         l[i] += __shfl_xor(l[i], 16);
@@ -297,9 +297,9 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
     if (threadIdx.x < ROWS) {
         float mt = -INFINITY, sum = 0.f;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) mt = fmaxf(mt, ml[0][w][threadIdx.x]);
+        for (int w = 0; w < WAVES; ++w) mt = fmaxf(mt, ml[0][w][threadIdx.x]);
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
+        for (int w = 0; w < WAVES; ++w) {
             const float mw = ml[0][w][threadIdx.x];
             sum += mw == -INFINITY ? ml[1][w][threadIdx.x] : ml[1][w][threadIdx.x] * __builtin_amdgcn_exp2f(mw - mt);    // (no maximum: 0, or NaN)
         }
@@ -318,11 +318,11 @@ template <int DT, int NW, int NT> __global__ __launch_bounds__(256) void k_cache
             for (int f = 0; f < FT; ++f) sums[(col * (DP + 4) + 16 * f + 4 * grp) / 4] = acc[i][f] * back;
         }
         __syncthreads();
-        for (int x = threadIdx.x; x < min(16, rows_here - 16 * i) * (DP / 4); x += 256) {
+        for (int x = threadIdx.x; x < min(16, rows_here - 16 * i) * (DP / 4); x += 64 * WAVES) {
             const int cl = x / (DP / 4), f = x % (DP / 4) * 4, row = row0 + 16 * i + cl;
             f32x4 o = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < 4; ++w) o += ((const f32x4 *)(lds + w * WAVE_BYTES))[(cl * (DP + 4) + f) / 4];
+            for (int w = 0; w < WAVES; ++w) o += ((const f32x4 *)(lds + w * WAVE_BYTES))[(cl * (DP + 4) + f) / 4];
             if (a.splits > 1) {
                 *(f32x4 *)(pt + (16 * i + cl) * DP + f) = o;
                 if (f == 0) pt[ROWS * DP + 16 * i + cl] = total[0][16 * i + cl], pt[ROWS * DP + ROWS + 16 * i + cl] = total[1][16 * i + cl];
@@ -394,7 +394,13 @@ template <int DT> __global__ __launch_bounds__(128) void k_cache_join(CacheFew f
 namespace {
 template <int DT, int NW, int NT> void few(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_cache_few<DT, NW, NT>), cache_grid(g, c, p), dim3(256), 0, s, args, dev, g, c, p.part);
+    if constexpr (NW <= 4) {
+        if (p.eight) {
+            hipLaunchKernelGGL((k_cache_few<DT, NW, NT, 8>), cache_grid(g, c, p), dim3(512), 0, s, args, dev, g, c, p.part);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((k_cache_few<DT, NW, NT, 4>), cache_grid(g, c, p), dim3(256), 0, s, args, dev, g, c, p.part);
 }
 template <int NW> void few_of(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
