@@ -1,5 +1,5 @@
 // The user cache's pages: rows in and out, table entries, whole pages moved (include/aif_cache.h).
-// All of it is data movement, and memory bounds it (16 histories of 20,011 rows, two heads of 128 in fp32: appended in 156 us, 4.8 TB/s; calls of few
+// All of it is data movement, and memory bounds it (16 histories of 20,011 rows, two heads of 128 in fp32: appended in 151 us, 4.9 TB/s; calls of few
 // rows, the launch).  A thread takes eight features of a row, which is four bytes of codes; the four threads of a
 // block of 32 features find its largest magnitude among themselves.
 #include "aif_cache_dev.h"
