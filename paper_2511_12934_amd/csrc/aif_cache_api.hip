@@ -33,7 +33,7 @@ struct aif_cache_ctx {
     int device = 0;
     CacheBook book;
     int n_cu = 256;
-    float *part[2] = {};                    // partial results of the attention kernels for few and for many rows
+    float *part = nullptr;                  // partial results of one attention kernel, which are joined before the next one starts
     std::vector<uint32_t> stamp;            // sequences that a call has named
     uint32_t stamp_now = 0;
     // Pinned memory for descriptors, in two halves.  Calls take pieces of one half until it is full; an event then marks the work that reads it,
@@ -311,8 +311,7 @@ void cdestroy(aif_cache_ctx *c)
 {
     if (!c) return;
     if (c->shape.table) (void)hipFree(c->shape.table);
-    for (float *p : c->part)
-        if (p) (void)hipFree(p);
+    if (c->part) (void)hipFree(c->part);
     if (c->d_stage) (void)hipFree(c->d_stage);
     if (c->h_stage) (void)hipHostFree(c->h_stage);
     for (hipEvent_t e : c->ev)
@@ -361,7 +360,7 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
     int n_cu = 0;
     CACHE_TRY(nullptr, hipDeviceGetAttribute(&n_cu, hipDeviceAttributeMultiprocessorCount, c->device));
     if (n_cu > 0) c->n_cu = n_cu;
-    for (float *&p : c->part) CACHE_TRY(nullptr, hipMalloc((void **)&p, cache_part_floats(c->n_cu * PART_ROWS, s.dp) * sizeof(float)));
+    CACHE_TRY(nullptr, hipMalloc((void **)&c->part, cache_part_floats(c->n_cu * PART_ROWS, s.dp) * sizeof(float)));
     c->list.resize(std::max(CACHE_LIST_BYTES, outs_bytes(f->max_requests)));
     c->half_bytes = (std::max(2 * CACHE_LIST_BYTES, 4 * attend_bytes(f->max_requests)) + 255) / 256 * 256;        // (a list of asks is one, whatever its length)
     CACHE_TRY(nullptr, staging_alloc(c->half_bytes * 2, &c->h_stage, &c->h_stage_dev));
@@ -517,7 +516,7 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
 // of 64 over 800 keys 18.7 and 15.2).  Heads above 128 have no registers for it.  One query of each user over LONG_READ tiles a compute unit or more is a matter
 // of memory alone, which blocks of four ask more evenly (16 users, four heads of 128 over 131,072 keys 200 us, 208; over 65,536 107 and 104).
 //
-// Partial results have room for PART_ROWS rows a compute unit and kernel: keys / chunk is rounded, by a third up at most where that makes two or
+// Partial results have room for PART_ROWS rows a compute unit: keys / chunk is rounded, by a third up at most where that makes two or
 // more, and tiles * keys / chunk <= work / chunk <= 3 / 4 of the room.
 static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays, CachePlan &plan, size_t &bytes)
 {
@@ -599,7 +598,7 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         // entries of as many units: a row of the grid each, in which a block need not look for its entry (empty blocks in the place of missing units leave
         // whole XCDs without work)
         p.each = most_units * n == units && most_units <= 65535 ? (int32_t)most_units : 0;
-        p.part = c->part[kind];
+        p.part = c->part;
     }
     return true;
 }
