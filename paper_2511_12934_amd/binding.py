@@ -548,12 +548,16 @@ def _declare_cache(lib):
 
 
 def _row_stride(t, width: int) -> int:
-    """Elements from one row of [rows, ...] to the next; rows themselves lie close."""
-    if t is None or t.numel() == 0 or t.shape[0] == 1:
+    """Elements from one row of [rows, ...] to the next, 0 where there is one; rows themselves lie close."""
+    if t is None or t.numel() == 0:
         return 0
     row = t[0]
     if row.numel() != width or not row.is_contiguous():
         raise ValueError(f"a row of {width} contiguous features is wanted, got {tuple(row.shape)} with strides {row.stride()}")
+    if t.shape[0] == 1:
+        return 0
+    if t.stride(0) < width:                        # (a broadcast row: 0, which would say that rows lie close)
+        raise ValueError(f"rows of {width} features overlap: {tuple(t.shape)} with strides {t.stride()}")
     return int(t.stride(0))
 
 
