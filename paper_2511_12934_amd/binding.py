@@ -191,6 +191,11 @@ def _stream() -> Optional[int]:
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device()) or None
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
 class Request:
     """Device tensors of one request (or mini-batch slice)."""
 
@@ -561,6 +566,11 @@ def _row_stride(t, width: int) -> int:
     return int(t.stride(0))
 
 
+def _facts(width: int, **tensors):
+    """(name, features of a row, type, device) of every tensor that holds something: what a context is held against."""
+    return [(name, width, t.dtype, t.device) for name, t in tensors.items() if t is not None] if width else []
+
+
 class CacheAppend:
     """Rows for the end of a sequence: keys and vals [n_rows, n_kv_heads * d_head] (or [n_rows, n_kv_heads, d_head]), rows
     that may lie apart."""
@@ -576,6 +586,9 @@ class CacheAppend:
     def fill(self, r: aif_cache_append_req):
         r.seq, r.n_rows, r.keys, r.vals = self.seq, self.n_rows, _ptr(self.keys), _ptr(self.vals)
         r.key_stride, r.val_stride = self.strides
+
+    def facts(self):
+        return _facts(self.width, keys=self.keys, vals=self.vals)
 
 
 class CacheQuery:
@@ -599,6 +612,12 @@ class CacheQuery:
         r.q_stride, r.out_stride = self.strides
         r.sinks, r.window = self.sinks, self.window
 
+    def facts(self):
+        facts = _facts(self.width, q=self.q, out=self.out) + _facts(min(self.n_q, 1), positions=self.positions)
+        if self.lse is not None and self.n_q:
+            facts.append(("lse", self.lse.numel() // self.n_q, self.lse.dtype, self.lse.device))
+        return facts
+
 
 class CacheRead:
     """Rows [first, first + n_rows) of a sequence, to keys_out and vals_out [n_rows, ...] (either may be None)."""
@@ -617,11 +636,20 @@ class CacheRead:
         r.keys_out, r.vals_out = _ptr(self.keys_out), _ptr(self.vals_out)
         r.key_stride, r.val_stride = self.strides
 
+    def facts(self):
+        return _facts(self.width, keys_out=self.keys_out, vals_out=self.vals_out)
+
 
 def _pack_cache(kind, reqs):
+    """The array, which knows how many requests it holds and which tensors they have: each fact with the first request it is of."""
     arr = (kind * max(len(reqs), 1))()
+    facts = {}
     for i, q in enumerate(reqs):
         q.fill(arr[i])
+        for fact in q.facts():
+            if fact not in facts:
+                facts[fact] = i
+    arr.n, arr.facts, arr.fits = len(reqs), facts, None
     return arr
 
 
@@ -661,13 +689,19 @@ class CacheContext:
                  max_len: int, max_requests: int, max_queries: int = 1, scale: float = 0.0, n_pages: Optional[int] = None):
         self._lib = load()
         self._h = C.c_void_p()
+        self._check_pool(pool, _current_device())
         self._page_bytes = cache_page_bytes(dtype=dtype, n_heads=n_heads, n_kv_heads=n_kv_heads, d_head=d_head, page_len=page_len)
         have = pool.numel() * pool.element_size() // self._page_bytes
         n_pages = have if n_pages is None else n_pages
         if n_pages > have:
             raise ValueError(f"the pool holds {have} pages, not {n_pages}")
-        self._kv_width, self._q_width = n_kv_heads * d_head, n_heads * d_head
+        import torch
         self.n_heads, self.dtype = n_heads, dtype
+        kind = torch.float32 if dtype == AIF_F32 else torch.bfloat16
+        kv, q = (n_kv_heads * d_head, kind, pool.device), (n_heads * d_head, kind, pool.device)
+        # what tensors of a name have to be: features of a row, type, device
+        self._fits = dict(keys=kv, vals=kv, keys_out=kv, vals_out=kv, q=q, out=q, lse=(n_heads, torch.float32, pool.device),
+                          positions=(1, torch.int32, pool.device))
         cfg = aif_cache_config(dtype, n_heads, n_kv_heads, d_head, scale, page_len, n_pages, max_seqs, max_len, max_requests, max_queries)
         self._keep = (pool,)                       # borrowed for the life of the context
         st = self._lib.aif_cache_init(C.byref(cfg), _ptr(pool), C.byref(self._h))
@@ -679,36 +713,38 @@ class CacheContext:
         if st != AIF_OK:
             raise AifError(st, self._lib.aif_cache_last_error(self._h).decode())
 
-    def _packed(self, reqs, packed, pack, width, *tensors):
-        """The packed array; requests that are packed here are held against the context's row width and type first."""
-        if packed is not None:
-            return packed
-        import torch
-        want = torch.float32 if self.dtype == AIF_F32 else torch.bfloat16
-        for i, r in enumerate(reqs):
-            for name in tensors:
-                t = getattr(r, name)
-                if t is not None and t.numel() and (t.dtype != want or r.width != width):
-                    raise ValueError(f"request {i}: {name} has rows of {r.width} {t.dtype}, the context {width} {want}")
-        return pack(reqs)
+    def _packed(self, reqs, packed, pack):
+        """The packed array, its tensors held against the context's row widths, type and device, once.  (An array that was
+        not made by pack_cache_* is as its maker filled it.)"""
+        arr = pack(reqs) if packed is None else packed
+        facts = getattr(arr, "facts", None)
+        n = arr.n if facts is not None else len(arr) if isinstance(arr, C.Array) else len(reqs)
+        if len(reqs) > n:
+            raise ValueError(f"{len(reqs)} requests, {n} are packed")
+        if facts is None or arr.fits is self._fits:
+            return arr
+        for (name, *have), i in facts.items():
+            want = self._fits[name]
+            if tuple(have) == want:
+                continue
+            if name == "lse":
+                raise ValueError(f"request {i}: lse is [n_q, {self.n_heads}] fp32 on {want[2]}, has rows of {have[0]} {have[1]} on {have[2]}")
+            if name == "positions":
+                raise ValueError(f"request {i}: positions are int32 on {want[2]}, not {have[1]} on {have[2]}")
+            raise ValueError(f"request {i}: {name} has rows of {have[0]} {have[1]} on {have[2]}, the context {want[0]} {want[1]} on {want[2]}")
+        arr.fits = self._fits
+        return arr
 
     def aif_cache_append(self, reqs: Sequence[CacheAppend], packed=None):
-        arr = self._packed(reqs, packed, pack_cache_appends, self._kv_width, "keys", "vals")
+        arr = self._packed(reqs, packed, pack_cache_appends)
         self._check(self._lib.aif_cache_append(self._h, arr, len(reqs), _stream()))
 
     def aif_cache_attend(self, reqs: Sequence[CacheQuery], packed=None):
-        arr = self._packed(reqs, packed, pack_cache_queries, self._q_width, "q", "out")
-        if packed is None:
-            import torch
-            for i, r in enumerate(reqs):
-                if r.lse is not None and (r.lse.dtype != torch.float32 or r.lse.numel() != r.n_q * self.n_heads):
-                    raise ValueError(f"request {i}: lse is [n_q, {self.n_heads}] fp32")
-                if r.positions is not None and r.positions.dtype != torch.int32:
-                    raise ValueError(f"request {i}: positions are int32")
+        arr = self._packed(reqs, packed, pack_cache_queries)
         self._check(self._lib.aif_cache_attend(self._h, arr, len(reqs), _stream()))
 
     def aif_cache_read(self, reqs: Sequence[CacheRead], packed=None):
-        arr = self._packed(reqs, packed, pack_cache_reads, self._kv_width, "keys_out", "vals_out")
+        arr = self._packed(reqs, packed, pack_cache_reads)
         self._check(self._lib.aif_cache_read(self._h, arr, len(reqs), _stream()))
 
     def _pairs(self, src, dst):
@@ -739,7 +775,13 @@ class CacheContext:
         self._check(self._lib.aif_cache_compact(self._h, C.byref(n), _stream()))
         return n.value
 
+    @staticmethod
+    def _check_pool(pool, device):
+        if not pool.is_cuda or not pool.is_contiguous() or pool.device.index != device:
+            raise ValueError(f"the pool is contiguous memory of GPU {device}, not of {pool.device}")
+
     def aif_cache_swap_pool(self, pool, n_pages: Optional[int] = None):
+        self._check_pool(pool, self._keep[0].device.index)
         have = pool.numel() * pool.element_size() // self._page_bytes
         if n_pages is not None and n_pages > have:
             raise ValueError(f"the pool holds {have} pages, not {n_pages}")

@@ -49,3 +49,119 @@ def test_rows_that_are_taken(torch):
         width = t[0].numel() if t.shape[0] else 0
         assert B._row_stride(t, width) == stride
         assert B.CacheAppend(0, t, t).strides == B.CacheQuery(0, t, t).strides == B.CacheRead(0, t, t).strides == (stride, stride)
+
+
+class Calls:
+    """The library's sizes, and calls that only count."""
+
+    def __init__(self, real):
+        self.aif_cache_page_bytes, self.seen = real.aif_cache_page_bytes, []
+
+    def __getattr__(self, name):
+        def call(*args):
+            self.seen.append(name)
+            return B.AIF_OK
+        return call
+
+
+class Pool:
+    """A pool on the requests' device as far as the binding looks at it."""
+
+    def __init__(self, device, pages=4, cuda=True, close=True):
+        self.device, self.pages, self.is_cuda, self.close = device, pages, cuda, close
+
+    def numel(self):
+        return self.pages * B.cache_page_bytes(**SHAPE)
+
+    def element_size(self):
+        return 1
+
+    def is_contiguous(self):
+        return self.close
+
+    def data_ptr(self):
+        return 64
+
+
+SHAPE = dict(dtype=B.AIF_BF16, n_heads=4, n_kv_heads=2, d_head=16, page_len=32)
+
+
+@pytest.fixture
+def lib(monkeypatch):
+    calls = Calls(B.load())
+    monkeypatch.setattr(B, "load", lambda: calls)
+    monkeypatch.setattr(B, "_stream", lambda: None)
+    monkeypatch.setattr(B, "_current_device", lambda: None)
+    return calls
+
+
+def _context(torch, lib, **kw):
+    return B.CacheContext(pool=kw.pop("pool", Pool(torch.device("cpu"))), max_seqs=4, max_len=100, max_requests=8, max_queries=8, **{**SHAPE, **kw})
+
+
+@pytest.mark.parametrize("beforehand", (False, True))
+def test_requests_packed_beforehand_are_held_against_the_context_too(torch, lib, beforehand):
+    ctx = _context(torch, lib)
+    bf = lambda *s: torch.zeros(s, dtype=torch.bfloat16)  # noqa: E731
+    q, lse = bf(3, 4, 16), torch.zeros(3, 4)
+    append = (ctx.aif_cache_append, B.pack_cache_appends)
+    attend = (ctx.aif_cache_attend, B.pack_cache_queries)
+    reads = (ctx.aif_cache_read, B.pack_cache_reads)
+    fine = [(append, B.CacheAppend(0, bf(3, 2, 16), bf(3, 2, 16))),
+            (attend, B.CacheQuery(0, q, q, lse=lse, positions=torch.zeros(3, dtype=torch.int32))), (attend, B.CacheQuery(0, q[:0], q[:0])),
+            (attend, B.CacheQuery(0, q[:1], q[:1], lse=lse[:1])), (reads, B.CacheRead(0, None, bf(3, 32))), (reads, B.CacheRead(0, bf(3, 32), None))]
+    bad = [(append, "keys has rows of 32 torch.float32", B.CacheAppend(0, torch.zeros(3, 32), torch.zeros(3, 32))),
+           (append, "vals has rows of 32 torch.float32", B.CacheAppend(0, bf(3, 32), torch.zeros(3, 32))),
+           (append, "keys has rows of 64", B.CacheAppend(0, bf(3, 64), bf(3, 64))),
+           (append, "keys has rows of 32 torch.bfloat16 on meta", B.CacheAppend(0, bf(3, 32).to("meta"), bf(3, 32))),
+           (attend, "q has rows of 32", B.CacheQuery(0, bf(3, 2, 16), bf(3, 2, 16))),
+           (attend, "out has rows of 64 torch.float32", B.CacheQuery(0, q, q.float())),
+           (attend, "lse is", B.CacheQuery(0, q, q, lse=torch.zeros(3, 2))), (attend, "lse is", B.CacheQuery(0, q, q, lse=torch.zeros(3, 0))), (attend, "lse is", B.CacheQuery(0, q, q, lse=lse.double())),
+           (attend, "positions are int32", B.CacheQuery(0, q, q, positions=torch.zeros(3, dtype=torch.int64))),
+           (reads, "keys_out has rows of 16", B.CacheRead(0, bf(3, 16), None)), (reads, "vals_out has rows of 32 torch.float16", B.CacheRead(0, None, bf(3, 32).half()))]
+    lib.seen.clear()
+    for (call, pack), r in fine:
+        many = [r] * 3
+        call(many, packed=pack(many) if beforehand else None)
+        call(many[:2], **({"packed": pack(many)} if beforehand else {}))
+    assert len(lib.seen) == 2 * len(fine)
+    for (call, pack), word, r in bad:
+        many = [x for (c, _), x in fine if c == call][:1] + [r]
+        for _ in range(2):
+            with pytest.raises(ValueError, match="request 1: " + word):
+                call(many, packed=pack(many) if beforehand else None)
+    assert len(lib.seen) == 2 * len(fine)
+
+
+def test_a_packed_array_serves_the_contexts_that_it_fits(torch, lib):
+    a, b = _context(torch, lib), _context(torch, lib, n_kv_heads=4)
+    rows = [B.CacheAppend(0, torch.zeros(3, 32, dtype=torch.bfloat16), torch.zeros(3, 32, dtype=torch.bfloat16))]
+    packed = B.pack_cache_appends(rows)
+    for _ in range(2):
+        a.aif_cache_append(rows, packed=packed)
+        with pytest.raises(ValueError, match="rows of 32"):
+            b.aif_cache_append(rows, packed=packed)
+
+
+def test_more_requests_than_were_packed_are_refused(torch, lib):
+    ctx = _context(torch, lib)
+    x = torch.zeros(3, 32, dtype=torch.bfloat16)
+    r = B.CacheAppend(0, x, x)
+    lib.seen.clear()
+    for packed in (B.pack_cache_appends([r]), (B.aif_cache_append_req * 1)()):
+        with pytest.raises(ValueError, match="2 requests"):
+            ctx.aif_cache_append([r, r], packed=packed)
+    with pytest.raises(ValueError, match="1 requests"):
+        ctx.aif_cache_append([r], packed=B.pack_cache_appends([]))
+    assert not lib.seen
+
+
+def test_pools_refused(torch, lib):
+    cpu = torch.device("cpu")
+    for pool in (Pool(cpu, cuda=False), Pool(cpu, close=False)):
+        with pytest.raises(ValueError, match="pool"):
+            _context(torch, lib, pool=pool)
+        with pytest.raises(ValueError, match="pool"):
+            _context(torch, lib).aif_cache_swap_pool(pool)
+    with pytest.raises(ValueError, match="pool"):
+        _context(torch, lib).aif_cache_swap_pool(Pool(torch.device("cuda", 1)))
