@@ -552,6 +552,14 @@ def _declare_cache(lib):
         f.restype, f.argtypes = res, args
 
 
+def _i32(x) -> int:
+    """A whole number as the C fields hold it (ctypes keeps the low bits of a larger one)."""
+    x = int(x)
+    if not -1 << 31 <= x < 1 << 31:
+        raise ValueError(f"{x} does not fit in 32 bits")
+    return x
+
+
 def _row_stride(t, width: int) -> int:
     """Elements from one row of [rows, ...] to the next, 0 where there is one; rows themselves lie close."""
     if t is None or t.numel() == 0:
@@ -576,7 +584,7 @@ class CacheAppend:
     that may lie apart."""
 
     def __init__(self, seq: int, keys, vals):
-        self.seq, self.keys, self.vals = int(seq), keys, vals
+        self.seq, self.keys, self.vals = _i32(seq), keys, vals
         self.n_rows = int(keys.shape[0])
         if tuple(vals.shape) != tuple(keys.shape):
             raise ValueError(f"keys {tuple(keys.shape)} and vals {tuple(vals.shape)} differ")
@@ -596,8 +604,8 @@ class CacheQuery:
     lse [n_q, n_heads] fp32 and positions [n_q] int32, both contiguous."""
 
     def __init__(self, seq: int, q, out, lse=None, positions=None, sinks: int = 0, window: int = 0):
-        self.seq, self.q, self.out, self.lse, self.positions = int(seq), q, out, lse, positions
-        self.sinks, self.window = int(sinks), int(window)
+        self.seq, self.q, self.out, self.lse, self.positions = _i32(seq), q, out, lse, positions
+        self.sinks, self.window = _i32(sinks), _i32(window)
         self.n_q = int(q.shape[0])
         if tuple(out.shape) != tuple(q.shape):
             raise ValueError(f"q {tuple(q.shape)} and out {tuple(out.shape)} differ")
@@ -623,7 +631,7 @@ class CacheRead:
     """Rows [first, first + n_rows) of a sequence, to keys_out and vals_out [n_rows, ...] (either may be None)."""
 
     def __init__(self, seq: int, keys_out, vals_out, first: int = 0):
-        self.seq, self.keys_out, self.vals_out, self.first = int(seq), keys_out, vals_out, int(first)
+        self.seq, self.keys_out, self.vals_out, self.first = _i32(seq), keys_out, vals_out, _i32(first)
         one = keys_out if keys_out is not None else vals_out
         if one is None or (vals_out is not None and tuple(vals_out.shape) != tuple(one.shape)):
             raise ValueError("keys_out or vals_out is wanted, of one shape")
@@ -669,13 +677,13 @@ def cache_ids(seqs):
     """Sequence numbers as the array the C entry points take; such an array is taken as it is."""
     if isinstance(seqs, C.Array):
         return seqs
-    seqs = [int(q) for q in seqs]
+    seqs = [_i32(q) for q in seqs]
     return (C.c_int32 * len(seqs))(*seqs)
 
 
 def cache_page_bytes(*, dtype: int, n_heads: int, n_kv_heads: int, d_head: int, page_len: int) -> int:
     """Bytes of a page; the pool is n_pages of them."""
-    cfg = aif_cache_config(dtype, n_heads, n_kv_heads, d_head, 0.0, page_len, 0, 0, 0, 0, 0)
+    cfg = aif_cache_config(dtype, _i32(n_heads), _i32(n_kv_heads), _i32(d_head), 0.0, _i32(page_len), 0, 0, 0, 0, 0)
     n = int(load().aif_cache_page_bytes(C.byref(cfg)))
     if n == 0:
         raise AifError(AIF_ESHAPE, load().aif_cache_last_error(None).decode())
@@ -702,7 +710,8 @@ class CacheContext:
         # what tensors of a name have to be: features of a row, type, device
         self._fits = dict(keys=kv, vals=kv, keys_out=kv, vals_out=kv, q=q, out=q, lse=(n_heads, torch.float32, pool.device),
                           positions=(1, torch.int32, pool.device))
-        cfg = aif_cache_config(dtype, n_heads, n_kv_heads, d_head, scale, page_len, n_pages, max_seqs, max_len, max_requests, max_queries)
+        cfg = aif_cache_config(dtype, n_heads, n_kv_heads, d_head, scale, page_len, _i32(n_pages), _i32(max_seqs), _i32(max_len), _i32(max_requests),
+                               _i32(max_queries))
         self._keep = (pool,)                       # borrowed for the life of the context
         st = self._lib.aif_cache_init(C.byref(cfg), _ptr(pool), C.byref(self._h))
         if st != AIF_OK:
@@ -764,11 +773,11 @@ class CacheContext:
         self._check(self._lib.aif_cache_free(self._h, seqs, len(seqs)))
 
     def aif_cache_truncate(self, seq: int, length: int):
-        self._check(self._lib.aif_cache_truncate(self._h, seq, length))
+        self._check(self._lib.aif_cache_truncate(self._h, _i32(seq), _i32(length)))
 
     def aif_cache_trim(self, seqs, sinks: int, window: int):
         seqs = cache_ids(seqs)
-        self._check(self._lib.aif_cache_trim(self._h, seqs, len(seqs), sinks, window, _stream()))
+        self._check(self._lib.aif_cache_trim(self._h, seqs, len(seqs), _i32(sinks), _i32(window), _stream()))
 
     def aif_cache_compact(self) -> int:
         n = C.c_int32(0)
@@ -785,7 +794,7 @@ class CacheContext:
         have = pool.numel() * pool.element_size() // self._page_bytes
         if n_pages is not None and n_pages > have:
             raise ValueError(f"the pool holds {have} pages, not {n_pages}")
-        self._check(self._lib.aif_cache_swap_pool(self._h, _ptr(pool), have if n_pages is None else n_pages))
+        self._check(self._lib.aif_cache_swap_pool(self._h, _ptr(pool), have if n_pages is None else _i32(n_pages)))
         import torch
         for old in self._keep:                     # enqueued work may still read it: its memory is not given away before that has run
             if old.is_cuda:
@@ -793,7 +802,7 @@ class CacheContext:
         self._keep = (pool,)
 
     def aif_cache_len(self, seq: int) -> int:
-        return int(self._lib.aif_cache_len(self._h, seq))
+        return int(self._lib.aif_cache_len(self._h, seq if 0 <= seq < 1 << 31 else -1))
 
     def aif_cache_free_pages(self) -> int:
         return int(self._lib.aif_cache_free_pages(self._h))

@@ -165,3 +165,24 @@ def test_pools_refused(torch, lib):
             _context(torch, lib).aif_cache_swap_pool(pool)
     with pytest.raises(ValueError, match="pool"):
         _context(torch, lib).aif_cache_swap_pool(Pool(torch.device("cuda", 1)))
+
+
+@pytest.mark.parametrize("number", (2 ** 31, 2 ** 32, 2 ** 32 + 1, -2 ** 31 - 1))
+def test_numbers_beyond_32_bits_are_refused(torch, lib, number):
+    """(A C field keeps their low 32 bits without a word: 2^32 + 1 would be sequence 1, a window of 2^32 none.)"""
+    ctx = _context(torch, lib)
+    x = torch.zeros(3, 4, 16, dtype=torch.bfloat16)
+    lib.seen.clear()
+    for f in (lambda: B.CacheAppend(number, x, x), lambda: B.CacheQuery(number, x, x), lambda: B.CacheQuery(0, x, x, sinks=number),
+              lambda: B.CacheQuery(0, x, x, window=number), lambda: B.CacheRead(number, x, x), lambda: B.CacheRead(0, x, x, first=number),
+              lambda: B.cache_ids([0, number]), lambda: ctx.aif_cache_free([number]), lambda: ctx.aif_cache_fork([0], [number]),
+              lambda: ctx.aif_cache_truncate(number, 0), lambda: ctx.aif_cache_truncate(0, number), lambda: ctx.aif_cache_trim([0], number, 1),
+              lambda: ctx.aif_cache_trim([0], 0, number), lambda: ctx.aif_cache_swap_pool(Pool(torch.device("cpu")), number),
+              lambda: _context(torch, lib, page_len=number), lambda: B.CacheContext(pool=Pool(torch.device("cpu")), max_seqs=4, max_len=number, max_requests=8, **SHAPE),
+              lambda: B.CacheContext(pool=Pool(torch.device("cpu")), max_seqs=number, max_len=9, max_requests=8, **SHAPE)):
+        with pytest.raises(ValueError, match="32 bits|the pool holds"):
+            f()
+    assert set(lib.seen) <= {"aif_cache_destroy"}
+    lib.aif_cache_len = lambda h, seq: seq if seq >= 0 else -1
+    assert ctx.aif_cache_len(number) == -1 and ctx.aif_cache_len(3) == 3        # "outside the context"
+    assert list(B.cache_ids([5, 2 ** 31 - 1, -1])) == [5, 2 ** 31 - 1, -1] and B.CacheQuery(0, x, x, window=2 ** 31 - 1).window == 2 ** 31 - 1
