@@ -39,9 +39,12 @@
  * once; the pages' contents follow in the order of the stream, so calls on one
  * context belong on one stream, or on streams that the caller orders.  A
  * context serves one thread at a time.  Not capturable into a HIP graph: under
- * capture the calls that enqueue return AIF_EINVAL.  AIF_EDEVICE after a call
- * of several launches may leave the sequences that it names with rows that were
- * not written: free them.
+ * capture the calls that enqueue return AIF_EINVAL.
+ * AIF_EDEVICE: a HIP call failed, or the current device is another one.  In the
+ * second case nothing has changed.  In the first, outputs of attend and read
+ * hold anything, and what the device holds of the sequences that append and trim
+ * name, fork and copy make, or compact moves (any) is not known: these are empty
+ * afterwards.  The other sequences are as they were.
  */
 #ifndef AIF_CACHE_H
 #define AIF_CACHE_H

@@ -2,7 +2,7 @@
 //
 // The host's book-keeping is what counts: every call settles at once which pages it takes and gives back, and the device's
 // copy of the page table follows on the stream with the launches that need it.  A call checks everything first; from there on
-// only a HIP call can fail.  Nothing is allocated after aif_cache_init.
+// only a HIP call can fail, and what the call was changing is given up (settled).  Nothing is allocated after aif_cache_init.
 #include "../../include/aif_cache.h"
 #include "aif_cache_dev.h"
 #include "cache_book.h"
@@ -72,6 +72,13 @@ aif_status cfail(aif_cache_ctx *c, aif_status st, const char *fmt, ...)
                          hipGetErrorString(e_));                                                      \
     } while (0)
 
+// What a call enqueues once its arguments are found right: an error of any kind is the device's.
+#define CACHE_RUN(ctxp, expr)                                                                         \
+    do {                                                                                              \
+        hipError_t e_ = (expr);                                                                       \
+        if (e_ != hipSuccess) return cfail(ctxp, AIF_EDEVICE, "%s: %s", #expr, hipGetErrorString(e_)); \
+    } while (0)
+
 size_t bytes_of_page(const aif_cache_config *f)
 {
     return (size_t)f->n_kv_heads * (f->page_len / CACHE_TILE) * cache_tile_bytes((f->d_head + CACHE_BLOCK - 1) / CACHE_BLOCK * CACHE_BLOCK);
@@ -131,7 +138,7 @@ aif_status check_tensor(aif_cache_ctx *c, const char *what, int i, const void *p
 aif_status check_stream(aif_cache_ctx *c, hipStream_t s)
 {
     int cur = -1;
-    CACHE_TRY(c, hipGetDevice(&cur));
+    CACHE_RUN(c, hipGetDevice(&cur));
     if (cur != c->device) return cfail(c, AIF_EDEVICE, "context belongs to device %d, current device is %d", c->device, cur);
     hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
     if (hipStreamIsCapturing(s, &st) != hipSuccess) {       // the default stream while another one is captured
@@ -147,10 +154,10 @@ aif_status stage_take(aif_cache_ctx *c, size_t bytes, hipStream_t s, size_t &off
 {
     bytes = (bytes + 255) / 256 * 256;
     if (c->at + bytes > c->half_bytes) {
-        CACHE_TRY(c, hipEventRecord(c->ev[c->half], s));
+        CACHE_RUN(c, hipEventRecord(c->ev[c->half], s));
         c->ev_live[c->half] = true;
         const int other = c->half ^ 1;
-        if (c->ev_live[other]) CACHE_TRY(c, hipEventSynchronize(c->ev[other]));
+        if (c->ev_live[other]) CACHE_RUN(c, hipEventSynchronize(c->ev[other]));
         c->ev_live[other] = false;
         c->half = other;
         c->at = 0;
@@ -194,9 +201,9 @@ public:
         if (far_) {
             // a descriptor is read by one block, or one a head: from the pinned memory itself where that is mapped
             l.dev = c_->h_stage_dev ? c_->h_stage_dev + off_ : c_->d_stage + off_;
-            if (!c_->h_stage_dev) CACHE_TRY(c_, staging_upload(c_->h_stage, nullptr, off_, c_->d_stage + off_, l.bytes, s_));
+            if (!c_->h_stage_dev) CACHE_RUN(c_, staging_upload(c_->h_stage, nullptr, off_, c_->d_stage + off_, l.bytes, s_));
         }
-        CACHE_TRY(c_, go(l));
+        CACHE_RUN(c_, go(l));
         return AIF_OK;
     }
 
@@ -218,10 +225,10 @@ template <class F> aif_status send_list(aif_cache_ctx *c, const char *h, int n, 
         const aif_status st = stage_take(c, bytes, s, off);
         if (st != AIF_OK) return st;
         __builtin_memcpy(c->h_stage + off, h, bytes);
-        CACHE_TRY(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
+        CACHE_RUN(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
         l.dev = c->d_stage + off;
     }
-    CACHE_TRY(c, go(l));
+    CACHE_RUN(c, go(l));
     return AIF_OK;
 }
 
@@ -306,6 +313,15 @@ private:
     CacheRun *runs_;
     int n_ = 0, pages_ = 0;
 };
+
+// The end of a call that changed the book: where the device failed it, it is not known what the device holds of the sequences that the call changed.
+// They become empty, so that nobody reads it.
+aif_status settled(aif_cache_ctx *c, aif_status st, const int32_t *seqs, int32_t n)
+{
+    if (st != AIF_OK)
+        for (int i = 0; i < n; ++i) c->book.truncate(seqs[i], 0);
+    return st;
+}
 
 void cdestroy(aif_cache_ctx *c)
 {
@@ -448,6 +464,7 @@ aif_status aif_cache_append(aif_cache_ctx *c, const aif_cache_append_req *reqs, 
     }
     if (st == AIF_OK) st = ins.send();
     c->book.settle();
+    for (int r = 0; st != AIF_OK && r < n; ++r) c->book.truncate(reqs[r].seq, 0);       // (settled)
     return st;
 }
 
@@ -676,10 +693,10 @@ aif_status aif_cache_attend(aif_cache_ctx *c, const aif_cache_attend_req *reqs, 
         }
     }
     if (far) {
-        CACHE_TRY(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
+        CACHE_RUN(c, staging_upload(c->h_stage, c->h_stage_dev, off, c->d_stage + off, bytes, s));
         l.dev = c->d_stage + off;
     }
-    CACHE_TRY(c, launch_cache_attend(c->shape, l, plan, s));
+    CACHE_RUN(c, launch_cache_attend(c->shape, l, plan, s));
     return AIF_OK;
 }
 
@@ -716,7 +733,7 @@ aif_status aif_cache_fork(aif_cache_ctx *c, const int32_t *src, const int32_t *d
         const int np = c->book.pages(c->book.len(src[i]));
         if (np) st = batch.add(CacheFill{c->book.entry(dst[i], 0), np, c->book.entry(src[i], 0), 0}, go);
     }
-    return st == AIF_OK ? batch.send(go) : st;
+    return settled(c, st == AIF_OK ? batch.send(go) : st, dst, n);
 }
 
 aif_status aif_cache_copy(aif_cache_ctx *c, const int32_t *src, const int32_t *dst, int32_t n, void *hip_stream)
@@ -734,7 +751,7 @@ aif_status aif_cache_copy(aif_cache_ctx *c, const int32_t *src, const int32_t *d
         c->book.copy(src[i], dst[i], [&](int32_t p, int32_t, int32_t to) {
             if (st == AIF_OK) st = copies.add(c->book.entry(src[i], p), c->book.entry(dst[i], p), to);
         });
-    return st == AIF_OK ? copies.send() : st;
+    return settled(c, st == AIF_OK ? copies.send() : st, dst, n);
 }
 
 aif_status aif_cache_free(aif_cache_ctx *c, const int32_t *seqs, int32_t n)
@@ -777,7 +794,7 @@ aif_status aif_cache_trim(aif_cache_ctx *c, const int32_t *seqs, int32_t n, int3
         c->book.trim(seqs[i], sinks, window, lo, hi);
         if (lo < hi) st = batch.add(CacheFill{c->book.entry(seqs[i], lo), hi - lo, -1, -1}, go);
     }
-    return st == AIF_OK ? batch.send(go) : st;
+    return settled(c, st == AIF_OK ? batch.send(go) : st, seqs, n);
 }
 
 aif_status aif_cache_compact(aif_cache_ctx *c, int32_t *n_used, void *hip_stream)
@@ -794,6 +811,7 @@ aif_status aif_cache_compact(aif_cache_ctx *c, int32_t *n_used, void *hip_stream
         c->book.compact([&](int32_t from, int32_t to) { if (st == AIF_OK) st = batch.add(CacheMove{from, to, -1}, go); },
                         [&](int32_t q, int32_t i, int32_t to) { if (st == AIF_OK) st = batch.add(CacheMove{-1, to, c->book.entry(q, i)}, go); });
         if (st == AIF_OK) st = batch.send(go);
+        for (int32_t q = 0; st != AIF_OK && q < c->cfg.max_seqs; ++q) c->book.truncate(q, 0);        // (settled)
     }
     if (n_used) *n_used = c->book.n_pages - c->book.n_free;
     return st;

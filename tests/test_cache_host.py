@@ -1,5 +1,5 @@
 """The whole host side of the user cache on a queue in the place of the device (cache_host.cpp): rows are the addresses that they were given by,
-launches read their descriptors when their turn comes."""
+launches read their descriptors when their turn comes, and any HIP call can be made to fail."""
 import ctypes as C
 import os
 import random
@@ -9,6 +9,8 @@ import pytest
 
 from paper_2511_12934_amd import binding as B
 from paper_2511_12934_amd import build
+
+OUT_OF_MEMORY, LAUNCH_FAILURE = 2, 719      # hipError_t
 
 
 @pytest.fixture(scope="module")
@@ -178,4 +180,78 @@ def test_calls_one_after_the_other_without_waiting(lib, caches, mapped, seed):
         done[what] += 1
         waited += lib.host_waiting() < before           # a call that waited for earlier ones
     assert waited >= 4 and all(done.values()), (waited, done)
+    c.check()
+
+
+def _a_cache(caches, mapped=True):
+    """Sequences 0..5 of 40 to 200 rows; 6 a fork of 0; scattered pages; 7..15 empty."""
+    c = caches(seqs=16, longest=300, pages=60, requests=16, mapped=mapped)
+    for turn in range(4):
+        assert c.append([(s, 10 * (s + 1)) for s in range(6)]) == B.AIF_OK
+    assert c.branch("fork", [0], [6]) == B.AIF_OK
+    c.free([2])
+    return c
+
+
+CALLS = [("append", lambda c: c.append([(0, 5), (6, 40), (7, 90), (8, 0)]), (0, 6, 7, 8)),
+         ("append of many runs", lambda c: c.append([(s, 1 + 7 * s) for s in range(15)]), tuple(range(15))),
+         ("fork", lambda c: c.branch("fork", [1, 5], [7, 8]), (7, 8)), ("copy", lambda c: c.branch("copy", [1, 5], [7, 8]), (7, 8)),
+         ("trim", lambda c: c.trim([5, 4, 1], 10, 40), (5, 4, 1)), ("compact", lambda c: c.compact(), tuple(range(16)))]
+
+
+@pytest.mark.parametrize("error", (OUT_OF_MEMORY, LAUNCH_FAILURE))
+@pytest.mark.parametrize("what,call,lost", CALLS, ids=[x[0] for x in CALLS])
+def test_a_call_that_the_device_fails_leaves_what_it_changes_empty(lib, caches, what, call, lost, error):
+    failed = 0
+    for at in range(1, 8):
+        c = _a_cache(caches)
+        c.check()
+        lib.host_fail(at, error)
+        before = lib.host_calls()
+        st = call(c)
+        if lib.host_calls() < before + at:
+            assert st == B.AIF_OK
+            lib.host_fail(0, 0)
+            c.check()
+            break
+        assert st == B.AIF_EDEVICE and b"as the test asked" in lib.aif_cache_last_error(c.h)
+        failed += 1
+        lib.host_fail(0, 0)
+        for s in lost:
+            assert lib.aif_cache_len(c.h, s) == 0, (s, at)
+            c.rows[s] = []
+        assert c.free_pages() == c.pages - sum(-(-len(c.rows[s]) // c.pl) for s in range(16) if s != 6)     # (6 has the pages of 0, or is lost as 0 is)
+        assert c.append([(s, 45) for s in lost[:3]]) == B.AIF_OK       # the context goes on
+        c.check()
+    assert failed and at < 7
+
+
+@pytest.mark.parametrize("error", (OUT_OF_MEMORY, LAUNCH_FAILURE))
+def test_queries_and_reads_that_the_device_fails_change_nothing(lib, caches, error):
+    for call in (lambda c: c.attend([(0, 1), (5, 3)]), lambda c: c.read([(0, 1, 20), (6, 0, 40)])):
+        c = _a_cache(caches)
+        lib.host_fail(1, error)
+        assert call(c) == B.AIF_EDEVICE
+        lib.host_fail(0, 0)
+        assert call(c) == B.AIF_OK
+        c.check()
+
+
+def test_a_wait_for_the_descriptors_memory_that_fails(lib, caches):
+    """The record and the wait between the halves of it: nothing is enqueued, and the same call goes through afterwards."""
+    c = caches(seqs=400, longest=60, pages=900, requests=400)
+    assert c.append([(s, 33) for s in range(400)]) == B.AIF_OK
+    asks = [(s, 1 + s % 2) for s in range(400)]
+    waits = 0
+    while waits < 4:
+        before = lib.host_waiting()
+        for at in (1, 2):
+            lib.host_fail(at, OUT_OF_MEMORY)
+            calls = lib.host_calls()
+            st = c.attend(asks[:300 + waits])
+            assert lib.host_calls() >= calls + 1 and (st == B.AIF_OK) == (lib.host_calls() < calls + at)
+            assert st in (B.AIF_OK, B.AIF_EDEVICE)
+            lib.host_fail(0, 0)
+        assert c.attend(asks) == B.AIF_OK
+        waits += lib.host_waiting() < before
     c.check()
