@@ -64,7 +64,7 @@ typedef struct {
     int32_t n_heads;        /* query heads, a multiple of n_kv_heads; head h reads kv head h / (n_heads / n_kv_heads) */
     int32_t n_kv_heads;     /* heads of a key or value row                                           */
     int32_t d_head;         /* a multiple of 16 bytes in dtype, up to 256                            */
-    float scale;            /* of the scores, > 0; 0 stands for 1 / sqrt(d_head)                     */
+    float scale;            /* of the scores, > 0, up to 2.35e38; 0 stands for 1 / sqrt(d_head)      */
     int32_t page_len;       /* rows of a page: a multiple of 32, 32..1024; a page has up to 2^29 bytes */
     int32_t n_pages;        /* pages of the pool                                                     */
     int32_t max_seqs;       /* sequence numbers are 0 .. max_seqs - 1                                */

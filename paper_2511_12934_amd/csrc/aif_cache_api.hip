@@ -343,7 +343,7 @@ aif_status cinit(const aif_cache_config *f, void *pool, aif_cache_ctx *c)
         return cfail(nullptr, AIF_EINVAL, "non-positive size in aif_cache_config");
     if (f->max_len > CACHE_MAX_LEN) return cfail(nullptr, AIF_ESHAPE, "max_len %d is above %d", f->max_len, CACHE_MAX_LEN);
     if (f->max_requests > 65535) return cfail(nullptr, AIF_ESHAPE, "max_requests %d is above 65535", f->max_requests);
-    if (!(f->scale >= 0.f) || f->scale - f->scale != 0.f) return cfail(nullptr, AIF_EINVAL, "scale is negative or not finite");
+    if (!(f->scale >= 0.f && f->scale <= 2.35e38f)) return cfail(nullptr, AIF_EINVAL, "scale is negative or above 2.35e38");      // (its product with log2 e is finite)
     if (!pool || (uintptr_t)pool % 64) return cfail(nullptr, AIF_EINVAL, "the pool is NULL or not 64-byte aligned");
     c->cfg = *f;
     CacheShape &s = c->shape;

@@ -186,3 +186,13 @@ def test_numbers_beyond_32_bits_are_refused(torch, lib, number):
     lib.aif_cache_len = lambda h, seq: seq if seq >= 0 else -1
     assert ctx.aif_cache_len(number) == -1 and ctx.aif_cache_len(3) == 3        # "outside the context"
     assert list(B.cache_ids([5, 2 ** 31 - 1, -1])) == [5, 2 ** 31 - 1, -1] and B.CacheQuery(0, x, x, window=2 ** 31 - 1).window == 2 ** 31 - 1
+
+
+@pytest.mark.parametrize("scale,status", ((2.36e38, B.AIF_EINVAL), (3.4e38, B.AIF_EINVAL), (-1e-30, B.AIF_EINVAL)))
+def test_scales_that_no_score_in_powers_of_two_has_are_refused(scale, status):
+    """scale / ln 2 has to be a number."""
+    import ctypes as C
+    cfg = B.aif_cache_config(B.AIF_BF16, 4, 2, 16, scale, 32, 4, 2, 100, 2, 1)
+    out = C.c_void_p()
+    assert B.load().aif_cache_init(C.byref(cfg), 64, C.byref(out)) == status and not out.value
+    assert b"scale" in B.load().aif_cache_last_error(None)
