@@ -232,8 +232,10 @@ __device__ __forceinline__ RowOf row_of(const CacheShape &c, int kvh, int row)
     return RowOf{i, kvh * c.group + row - i * c.group};
 }
 
-// Values in LDS: rows of 2 dp bytes in pieces of 16, piece `at` of row `key` in the place of piece at ^ f(key), so that neither the eight rows whose pieces
-// are written together nor the four rows of which eight bytes a lane are read together meet in a bank.
+// Values in LDS: rows of 2 dp bytes in pieces of 16, piece `at` of row `key` in the place of piece at ^ f(key).  Pieces that are written together do not
+// meet in a bank.  The turned reads, which could take 2 cycles a wave, take by the addresses 2 for odd dp / 32; in the row tiles of 16 and 32 2 for dp 64 and 192 and
+// 4 for 128 and 256, whose piece 2 f of row r lies where piece 2 f + 1 of row r ^ 1 would; in the larger ones, which ask for four pieces of four rows, 4 and 8.
+// The counters say the same: 2 cycles more for each read at dp 128 in the small tiles and at dp 64 in the large ones, a quarter of the LDS' active cycles.
 template <int DP> __device__ __forceinline__ int v_place(int key, int at) { return key * (2 * DP) + (at ^ (DP % 64 ? key / 2 % 4 : key % 8)) * 16; }
 // Where a lane's eight bytes of the turned read lie (four keys of one feature come back): keys key0 + lane % 16 / 4, 16 features from feature0 on
 // (both multiples of 4 and 16).

@@ -7,7 +7,7 @@
 // the vector ALU: per score one fused multiply-add, half a maximum, one exponential (2.3 times a plain instruction), half a conversion and one
 // addition.  Heads of 64: eight waves of 32 rows, four waves a SIMD (64 x 10^4 rows over 500 keys 121 us, 0.68
 // PFLOP/s; four waves of 64 rows that each bring the keys over for themselves, k_cache_own.hip, 130).
-// Rows of K are 16 bytes longer than their features: the lanes of a read meet different banks (V: v_place).
+// Rows of K are 16 bytes longer than their features, so that the lanes of a read meet in no bank; those of V do where heads are a multiple of 64 (v_place).
 #include "k_cache_attend.h"
 
 namespace aif {
