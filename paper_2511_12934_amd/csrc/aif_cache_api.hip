@@ -199,7 +199,8 @@ public:
         CacheList l{at_, nullptr, n_, (size_t)n_ * sizeof(T)};
         n_ = 0;
         if (far_) {
-            // a descriptor is read by one block, or one a head: from the pinned memory itself where that is mapped
+            // read by each of a descriptor's blocks -- k_cache_move: one for 16 KB of a page, k_cache_fill: one for 256 table entries -- from the pinned
+            // memory itself where that is mapped
             l.dev = c_->h_stage_dev ? c_->h_stage_dev + off_ : c_->d_stage + off_;
             if (!c_->h_stage_dev) CACHE_RUN(c_, staging_upload(c_->h_stage, nullptr, off_, c_->d_stage + off_, l.bytes, s_));
         }
