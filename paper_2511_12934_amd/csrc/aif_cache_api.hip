@@ -18,7 +18,7 @@ using namespace aif;
 
 namespace {
 constexpr size_t CACHE_LIST_BYTES = 512 << 10;      // of one launch's descriptors, at most
-constexpr int FEW_ROWS = 64, ROWS_OF_CU = 64, MIN_TILES = 4, LONG_READ = 768, MAX_SPLITS = 128, PART_ROWS = 384;      // plan_attend
+constexpr int FEW_ROWS = 64, ROWS_OF_CU = 64, MIN_TILES = 4, MAX_SPLITS = 128, PART_ROWS = 384;      // plan_attend
 constexpr int MAX_UNITS = (1 << 23) - 1;    // of up to 512 threads: a grid holds fewer than 2^32 along an axis
 constexpr int CACHE_MAX_LEN = 1 << 30;      // row numbers and sums of two of them fit in 32 bits
 constexpr int CACHE_MAX_PAGES = 1 << 23;    // of a sequence, and
@@ -533,8 +533,9 @@ aif_status aif_cache_read(aif_cache_ctx *c, const aif_cache_read_req *reqs, int3
 //
 // Waves.  Eight to a block of few rows take 0.62 times as long for a tile, but start and end later and are worth less beside another block (32 users x 128
 // queries, two heads of 128: over 200 keys 11.2 us with eight and 9.6 with four, over 800 14.0 and 16.4, over 3,000 25.3 and 33.5; 512 queries, a head
-// of 64 over 800 keys 18.7 and 15.2).  Heads above 128 have no registers for it.  One query of each user over LONG_READ tiles a compute unit or more is a matter
-// of memory alone, which blocks of four ask more evenly (16 users, four heads of 128 over 131,072 keys 200 us, 208; over 65,536 107 and 104).
+// of 64 over 800 keys 18.7 and 15.2).  Heads above 128 have no registers for it.  Where
+// memory alone counts they are about even: one query of each of 16 users, four heads over 3.3 to 6.7 MB a compute unit takes eight waves 0.95 to 1.04 of four's time with
+// heads of 128, 0.97 to 1.01 with heads of 64 and 0.99 to 1.01 with heads of 32.
 //
 // Partial results have room for PART_ROWS rows a compute unit: keys / chunk is rounded, by a third up at most where that makes two or
 // more, and tiles * keys / chunk <= work / chunk <= 3 / 4 of the room.
@@ -574,7 +575,7 @@ static bool plan_attend(aif_cache_ctx *c, CacheAsk *asks, int n, int32_t *arrays
         const double row_of_part = sh.dp * 8 / 1.8e6;
         int64_t chunk = std::max<int64_t>(longest, 1);
         double best = 0;
-        const bool may = kind == 0 && sh.dp <= 128 && !(sh.dtype == 1 && rows == 16 && work > (int64_t)LONG_READ * c->n_cu);
+        const bool may = kind == 0 && sh.dp <= 128;
         for (int eight = 0; eight <= may; ++eight) {
             const double start = eight ? (sh.dtype == 0 ? 1.5 : 0.8) : 0.0, one = eight ? 0.62 * tile : tile, beside = eight ? 1.37 : 0.8;
             auto time = [&](int64_t k, int64_t cut) {           // cut: blocks, of up to k tiles
