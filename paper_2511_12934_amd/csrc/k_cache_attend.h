@@ -25,7 +25,7 @@ struct CacheGrid {
 inline dim3 cache_grid(const CacheGrid &g, const CacheShape &c, const CachePart &p) { return p.each ? dim3(g.n, c.n_kv, p.each) : dim3(p.units, c.n_kv, 1); }
 
 void launch_cache_own(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
-void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
+hipError_t launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s);
 
 __device__ __forceinline__ CacheAsk ask_at(const char *dev, const CacheGrid &g, int r)
 {

@@ -433,10 +433,11 @@ hipError_t launch_cache_attend(const CacheShape &c, const CacheList &asks, const
         const CachePart &of = kind ? p.many : p.few;
         if (of.units == 0) continue;
         g.each = of.each;
+        hipError_t e = hipSuccess;
         if (kind && of.own) launch_cache_own(args, asks.dev, g, c, of, s);
-        else if (kind) launch_cache_many(args, asks.dev, g, c, of, s);
+        else if (kind) e = launch_cache_many(args, asks.dev, g, c, of, s);
         else launch_cache_few(args, asks.dev, g, c, of, s);
-        const hipError_t e = hipGetLastError();
+        if (e == hipSuccess) e = hipGetLastError();
         if (e != hipSuccess) return e;
         g.firsts += 4 * (asks.n + 1);
         if (of.joins) {

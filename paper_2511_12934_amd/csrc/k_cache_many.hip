@@ -249,7 +249,7 @@ template <int NW> void many_of(const CacheFew &args, const char *dev, const Cach
 
 }  // namespace
 
-void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
+hipError_t launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g, const CacheShape &c, const CachePart &p, hipStream_t s)
 {
     switch (c.dp / 32) {
     case 2: many_of<2>(args, dev, g, c, p, s); break;
@@ -258,8 +258,10 @@ void launch_cache_many(const CacheFew &args, const char *dev, const CacheGrid &g
     case 5: many_of<5>(args, dev, g, c, p, s); break;
     case 6: many_of<6>(args, dev, g, c, p, s); break;
     case 7: many_of<7>(args, dev, g, c, p, s); break;
-    default: many_of<8>(args, dev, g, c, p, s); break;
+    case 8: many_of<8>(args, dev, g, c, p, s); break;
+    default: return hipErrorInvalidValue;       // (heads of up to 32 are k_cache_own's)
     }
+    return hipGetLastError();
 }
 
 }  // namespace aif
