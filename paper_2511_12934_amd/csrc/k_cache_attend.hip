@@ -12,7 +12,7 @@
 // product's operand where they are, O^T = V^T P^T.  V has to be turned, features to rows: bf16 rows of 32 keys in the wave's own LDS,
 // read back by ds_read_b64_tr_b16 (four keys of one feature a lane; which lanes meet in a bank: v_place).  No barrier in the loop; the four or eight waves of a block take the tiles in turn, each
 // with the next tile's codes already asked for, and join through LDS.  16 users' histories of 131,072 behaviours, 4 kv heads of 128, one query of 16 heads:
-// 201 us, 5.7 TB/s.  With 32 rows to a tile conversions, products and softmax take as long as the bytes do: 0.25 us a tile and block at heads of 128, the bytes
+// 207 us, 5.5 TB/s.  With 32 rows to a tile conversions, products and softmax take as long as the bytes do: 0.25 us a tile and block at heads of 128, the bytes
 // at that rate 0.20.  Short calls take the launch, 4 us of loads one behind the other (arguments, table, codes), and the
 // join's launch where keys are split.
 #include "k_cache_attend.h"
