@@ -560,23 +560,34 @@ def _i32(x) -> int:
     return x
 
 
+def _row_width(t) -> int:
+    """Features of a row of [rows, ...]; 0 where there are no rows."""
+    return t.numel() // t.shape[0] if t.shape[0] else 0
+
+
 def _row_stride(t, width: int) -> int:
     """Elements from one row of [rows, ...] to the next, 0 where there is one; rows themselves lie close."""
     if t is None or t.numel() == 0:
         return 0
+    n = t.shape[0]
+    if t.is_contiguous() and t.numel() == n * width:
+        return width if n > 1 else 0
     row = t[0]
     if row.numel() != width or not row.is_contiguous():
         raise ValueError(f"a row of {width} contiguous features is wanted, got {tuple(row.shape)} with strides {row.stride()}")
-    if t.shape[0] == 1:
+    if n == 1:
         return 0
     if t.stride(0) < width:                        # (a broadcast row: 0, which would say that rows lie close)
         raise ValueError(f"rows of {width} features overlap: {tuple(t.shape)} with strides {t.stride()}")
     return int(t.stride(0))
 
 
-def _facts(width: int, **tensors):
-    """(name, features of a row, type, device) of every tensor that holds something: what a context is held against."""
-    return [(name, width, t.dtype, t.device) for name, t in tensors.items() if t is not None] if width else []
+def _kind(width: int, t):
+    return None if t is None else (width, t.dtype, t.device)
+
+
+def _like(t):
+    return None if t is None else (t.dtype, t.get_device())
 
 
 class CacheAppend:
@@ -588,15 +599,22 @@ class CacheAppend:
         self.n_rows = int(keys.shape[0])
         if tuple(vals.shape) != tuple(keys.shape):
             raise ValueError(f"keys {tuple(keys.shape)} and vals {tuple(vals.shape)} differ")
-        self.width = keys[0].numel() if self.n_rows else 0
+        self.width = _row_width(keys)
         self.strides = _row_stride(keys, self.width), _row_stride(vals, self.width)
 
     def fill(self, r: aif_cache_append_req):
         r.seq, r.n_rows, r.keys, r.vals = self.seq, self.n_rows, _ptr(self.keys), _ptr(self.vals)
         r.key_stride, r.val_stride = self.strides
 
-    def facts(self):
-        return _facts(self.width, keys=self.keys, vals=self.vals)
+    names = ("keys", "vals")
+
+    def kinds(self):
+        """What a context holds against its own: (features of a row, type, device) of each of `names`."""
+        return _kind(self.width, self.keys), _kind(self.width, self.vals)
+
+    def like(self):
+        """Alike where kinds() are, and quicker."""
+        return self.width, _like(self.keys), _like(self.vals)
 
 
 class CacheQuery:
@@ -612,7 +630,7 @@ class CacheQuery:
         for name, t, n in (("lse", lse, None), ("positions", positions, self.n_q)):
             if t is not None and (t.shape[0] != self.n_q or not t.is_contiguous() or (n is not None and t.numel() != n)):
                 raise ValueError(f"{name}: contiguous, a row for each of {self.n_q} queries, got {tuple(t.shape)}")
-        self.width = q[0].numel() if self.n_q else 0
+        self.width = _row_width(q)
         self.strides = _row_stride(q, self.width), _row_stride(out, self.width)
 
     def fill(self, r: aif_cache_attend_req):
@@ -620,11 +638,15 @@ class CacheQuery:
         r.q_stride, r.out_stride = self.strides
         r.sinks, r.window = self.sinks, self.window
 
-    def facts(self):
-        facts = _facts(self.width, q=self.q, out=self.out) + _facts(min(self.n_q, 1), positions=self.positions)
-        if self.lse is not None and self.n_q:
-            facts.append(("lse", self.lse.numel() // self.n_q, self.lse.dtype, self.lse.device))
-        return facts
+    names = ("q", "out", "lse", "positions")
+
+    def kinds(self):
+        lse = self.lse
+        return _kind(self.width, self.q), _kind(self.width, self.out), None if lse is None else _kind(_row_width(lse), lse), _kind(1, self.positions)
+
+    def like(self):
+        lse = self.lse
+        return self.width, _like(self.q), _like(self.out), None if lse is None else (lse.dtype, lse.get_device(), lse.numel() // self.n_q), _like(self.positions)
 
 
 class CacheRead:
@@ -636,7 +658,7 @@ class CacheRead:
         if one is None or (vals_out is not None and tuple(vals_out.shape) != tuple(one.shape)):
             raise ValueError("keys_out or vals_out is wanted, of one shape")
         self.n_rows = int(one.shape[0])
-        self.width = one[0].numel() if self.n_rows else 0
+        self.width = _row_width(one)
         self.strides = _row_stride(keys_out, self.width), _row_stride(vals_out, self.width)
 
     def fill(self, r: aif_cache_read_req):
@@ -644,20 +666,26 @@ class CacheRead:
         r.keys_out, r.vals_out = _ptr(self.keys_out), _ptr(self.vals_out)
         r.key_stride, r.val_stride = self.strides
 
-    def facts(self):
-        return _facts(self.width, keys_out=self.keys_out, vals_out=self.vals_out)
+    names = ("keys_out", "vals_out")
+
+    def kinds(self):
+        return _kind(self.width, self.keys_out), _kind(self.width, self.vals_out)
+
+    def like(self):
+        return self.width, _like(self.keys_out), _like(self.vals_out)
 
 
 def _pack_cache(kind, reqs):
-    """The array, which knows how many requests it holds and which tensors they have: each fact with the first request it is of."""
+    """The array, which knows how many requests it holds and of which kinds: the first of each run of requests of a kind."""
     arr = (kind * max(len(reqs), 1))()
-    facts = {}
+    runs, last = [], None
     for i, q in enumerate(reqs):
         q.fill(arr[i])
-        for fact in q.facts():
-            if fact not in facts:
-                facts[fact] = i
-    arr.n, arr.facts, arr.fits = len(reqs), facts, None
+        like = q.like() if q.width and len(reqs) > 1 else None
+        if q.width and (like is None or like != last):  # (a request without rows is of no kind)
+            runs.append((i, q.names, q.kinds()))
+            last = like
+    arr.n, arr.runs, arr.fits = len(reqs), runs, None
     return arr
 
 
@@ -726,21 +754,22 @@ class CacheContext:
         """The packed array, its tensors held against the context's row widths, type and device, once.  (An array that was
         not made by pack_cache_* is as its maker filled it.)"""
         arr = pack(reqs) if packed is None else packed
-        facts = getattr(arr, "facts", None)
-        n = arr.n if facts is not None else len(arr) if isinstance(arr, C.Array) else len(reqs)
+        runs = getattr(arr, "runs", None)
+        n = arr.n if runs is not None else len(arr) if isinstance(arr, C.Array) else len(reqs)
         if len(reqs) > n:
             raise ValueError(f"{len(reqs)} requests, {n} are packed")
-        if facts is None or arr.fits is self._fits:
+        if runs is None or arr.fits is self._fits:
             return arr
-        for (name, *have), i in facts.items():
-            want = self._fits[name]
-            if tuple(have) == want:
-                continue
-            if name == "lse":
-                raise ValueError(f"request {i}: lse is [n_q, {self.n_heads}] fp32 on {want[2]}, has rows of {have[0]} {have[1]} on {have[2]}")
-            if name == "positions":
-                raise ValueError(f"request {i}: positions are int32 on {want[2]}, not {have[1]} on {have[2]}")
-            raise ValueError(f"request {i}: {name} has rows of {have[0]} {have[1]} on {have[2]}, the context {want[0]} {want[1]} on {want[2]}")
+        for i, names, kinds in runs:
+            for name, have in zip(names, kinds):
+                want = self._fits[name]
+                if have is None or have == want:
+                    continue
+                if name == "lse":
+                    raise ValueError(f"request {i}: lse is [n_q, {self.n_heads}] fp32 on {want[2]}, has rows of {have[0]} {have[1]} on {have[2]}")
+                if name == "positions":
+                    raise ValueError(f"request {i}: positions are int32 on {want[2]}, not {have[1]} on {have[2]}")
+                raise ValueError(f"request {i}: {name} has rows of {have[0]} {have[1]} on {have[2]}, the context {want[0]} {want[1]} on {want[2]}")
         arr.fits = self._fits
         return arr
 
