@@ -140,6 +140,7 @@ aif_status aif_q8_rows(aif_q8_ctx *c, const aif_q8_rows_args *a, void *stream)
 {
     if (!c || !a) return qfail(c, AIF_EINVAL, "NULL argument");
     Q8_TRY(check_dtype(c, a->dtype, a->n_rows));
+    if (a->reserved) return qfail(c, AIF_EINVAL, "reserved field is not zero");
     Q8RowsCall r{};
     r.f32 = a->dtype == AIF_F32;
     Q8_TRY(check_width(c, "width", a->width, r.f32 && !a->q_out.codes ? 4 : 8, Q8_MAX_NORM));
@@ -172,6 +173,7 @@ aif_status aif_q8_linear(aif_q8_ctx *c, const aif_q8_linear_args *a, void *strea
 {
     if (!c || !a) return qfail(c, AIF_EINVAL, "NULL argument");
     Q8_TRY(check_dtype(c, a->dtype, a->n_rows));
+    if (a->reserved) return qfail(c, AIF_EINVAL, "reserved field is not zero");
     Q8LinearCall r{};
     r.f32 = a->dtype == AIF_F32;
     Q8_TRY(check_width(c, "k", a->k, 8, Q8_MAX_WIDTH));
