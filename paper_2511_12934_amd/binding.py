@@ -908,7 +908,8 @@ def _q8_dtype(t) -> int:
 
 class Q8Matrix:
     """A matrix of 8 bits: codes uint8 [rows, width] and scales uint8 [blocks of rows, blocks of columns or more], of one
-    device, rows that may lie apart.  block_rows: rows of a scale, 1 or 128 (a layer's weights)."""
+    device, rows that may lie apart.  block_rows: rows of a scale, 1 or 128 (a layer's weights).  A product reads rows of codes
+    up to a multiple of 16 bytes: the storage holds them, as q8_empty()'s does."""
 
     def __init__(self, codes, scales, block_rows: int = 1):
         import torch
@@ -949,6 +950,15 @@ def _q8_matrix(name, q, device, shape, block_rows):
     if tuple(q.codes.shape) != tuple(shape) or q.codes.device != device or q.block_rows != block_rows:
         raise ValueError(f"{name}: 8 bits {tuple(shape)} in blocks of {block_rows} rows on {device} are wanted, got {tuple(q.codes.shape)} of {q.block_rows} on {q.codes.device}")
     return q.c
+
+
+def _q8_operand(name, q, device, shape, block_rows):
+    """_q8_matrix() of what a product reads: rows of codes up to a multiple of 16 bytes, the last one's in its storage too."""
+    c, t = _q8_matrix(name, q, device, shape, block_rows), q.codes
+    end = t.storage_offset() + (q.rows - 1) * int(t.stride(0)) + -(-q.width // 16) * 16
+    if q.rows and end > t.untyped_storage().nbytes():
+        raise ValueError(f"{name}: a row of {q.width} codes is read up to a multiple of 16 bytes, the last one's end lies {end - t.untyped_storage().nbytes()} bytes behind its storage")
+    return c
 
 
 def _q8_vector(name, t, like, n):
@@ -997,9 +1007,9 @@ class Q8Linear(_Q8Call):
         like = None if typed is None else typed.dtype, device
         c = aif_q8_linear_args(dtype=dtype, n_rows=_i32(rows), k=_i32(k), n=_i32(n),
                                activation=AIF_Q8_GATE if up is not None else AIF_Q8_RELU if relu else AIF_Q8_NONE)
-        c.a, c.w = _q8_matrix("a", a, device, (rows, k), 1), _q8_matrix("w", w, device, (n, k), Q8_BLOCK)
+        c.a, c.w = _q8_operand("a", a, device, (rows, k), 1), _q8_operand("w", w, device, (n, k), Q8_BLOCK)
         if up is not None:
-            c.up = _q8_matrix("up", up, device, (n, k), Q8_BLOCK)
+            c.up = _q8_operand("up", up, device, (n, k), Q8_BLOCK)
         c.bias, c.residual = _q8_vector("bias", bias, like, n), _ptr(residual)
         c.residual_stride = _q8_rows("residual", residual, like, (rows, n))
         if isinstance(out, Q8Matrix):
