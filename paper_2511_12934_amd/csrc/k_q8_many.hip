@@ -18,6 +18,7 @@
 // 65536 x 4096 x 4096 with residual takes 951 us: a tile's 128 KB of results take about 5 us that its products do not hide; gated 16000 x 1024 x 4096 126 us (1.39 us a
 // step, 4.6 a tile's end, most of it exponentials and reciprocals), 32000 x 512 x 2048 in 8 bits 79 us.  Tried and slower: eight waves a tile of 256 by 256 (411 us for 8192^3), two blocks a unit with tiles of 128 by 256,
 // blocks started apart in time.  fp32 (bf16 products of whole codes) 4096 x 4096 x 4096 120 us, 1.15 PFLOP/s.
+#include "k_q8_form.h"
 #include "k_q8_product.h"
 #include "mfma_util.h"
 
@@ -451,27 +452,11 @@ template <int WM, int MT, int NG, bool GATE, bool WHOLE> hipError_t go(const Q8L
 hipError_t launch_q8_linear(const Q8LinearCall &c, int n_cu, hipStream_t s)
 {
     const bool gate = c.act == Q8_ACT_GATE;
-    // Small tiles as long as no unit gets many: 16 mt rows of them by 16 columns (8-bit results: 16 by 128) take a unit about 0.07 mt us for 128 columns of k,
-    // and a round of the large tiles takes 0.55 us (fp32: 0.95) for them however few the tiles are.  Large against small, us: 64 x 4096 x 4096 23.1 and
-    // 12.1, 64 x 1024 x 8192 (8 by this count) 8.6 and 6.4, 768 x 1024 x 1024 (12) 8.9 and 8.8, 64 x 1024 x 16384 (16) 9.1 and 12.6; fp32 512 x 1024 x 1024 (8) 12.4 and
-    // 7.1, 1000 x 1024 x 1024 (16) 12.9 and 12.9; gated with 8-bit results 256 x 1024 x 4096 (2 rounds) 14.5 and 11.3, 512 x 1024 x 4096 (4) 14.7 and 21.0.
-    const int64_t strips = c.out ? (c.n + 15) / 16 : (c.n + 127) / 128;
-    auto tiles = [&](int mt) { return ((int64_t)c.m + 16 * mt - 1) / (16 * mt) * strips; };
-    int mt = 1;                                                                  // as few rows as leave no unit two tiles
-    while (c.out && mt < 4 && c.m > 16 * mt && tiles(mt) > n_cu) mt *= 2;
-    if (((tiles(mt) + n_cu - 1) / n_cu) * mt <= (!c.out ? 2 : c.f32 ? 12 : 8)) return launch_q8_few(c, mt, s);
+    const Q8Form f = q8_form(c, n_cu);
+    if (f.few) return launch_q8_few(c, f.rows / 16, s);
     if (c.f32) return gate ? go<2, 4, 2, true, true>(c, n_cu, s) : go<2, 4, 1, false, true>(c, 2 * n_cu, s);
-    // Tiles of 256 by 256 or, two to a unit, of 128 by 128: a round of the large ones takes some 9 us and 1.1 - 1.4 us for each 128 columns of k, one of the small ones
-    // 6 and 1.05.  Large against small, us: 4096 x 4096 x 4096 (1 round, 2 rounds) 56 and 75, 32000 x 2048 x 512 with residual (1, 2) 46 and 56, 16000 x 2048 x 1024 (1, 2) 32 and
-    // 41, 2048 x 4096 x 4096 (1, 1) 45 and 40, 6000 x 1024 x 1024 (1, 1) 18.1 and 13.4, 20000 x 256 x 1024 (2, 3) 19.7 and 14.8.
-    // Where large ones leave a quarter of the units idle the small ones do as well or better: 10000 x 1024 x 1024 in 8 bits (160 tiles) 19.0 and 20.9 over and over, with the
-    // layer to 512 columns that reads it behind each 37.1 and 35.6.
-    // With a gate of 256 or 128 rows by 128 columns, one to a unit: 6000 x 1024 x 1024 (1, 2) 18.1 and 26.4, 10000 x 1024 x 1024 (2, 3) 30.5 and 34.7.
-    auto tiles_of = [&](int rows, int cols) { return ((int64_t)c.m + rows - 1) / rows * ((c.n + cols - 1) / cols); };
-    auto rounds = [&](int rows, int cols, int units) { return (tiles_of(rows, cols) + units - 1) / units; };
-    if (gate) return rounds(256, 128, n_cu) < rounds(128, 128, n_cu) ? go<4, 4, 2, true, false>(c, n_cu, s) : go<2, 4, 2, true, false>(c, n_cu, s);
-    const bool large = 4 * tiles_of(256, 256) >= 3 * (int64_t)n_cu && 8 * rounds(256, 256, n_cu) <= 5 * rounds(128, 128, 2 * n_cu);
-    return large ? go<2, 8, 2, false, false>(c, n_cu, s) : go<2, 4, 1, false, false>(c, 2 * n_cu, s);
+    if (gate) return f.rows == 256 ? go<4, 4, 2, true, false>(c, n_cu, s) : go<2, 4, 2, true, false>(c, n_cu, s);
+    return f.rows == 256 ? go<2, 8, 2, false, false>(c, n_cu, s) : go<2, 4, 1, false, false>(c, 2 * n_cu, s);
 }
 
 }  // namespace aif
