@@ -35,7 +35,7 @@ inline Q8Form q8_form(const Q8LinearCall &c, int n_cu)
     //   24576 x 1024 (384)                  256 19.8 and 17.1, 1024 33.1 and 34.7, 4096 100 and 128; in 8 bits 1024 42.4 and 38.3, 4096 107 and 130
     //   65536 x 1024 (1024)                 256 39.8 and 59.3; in 8 bits 256 55.3 and 51.3, 512 69.1 and 75.8
     //   with bias 10168 x 1752 (280)        1440 49.4 and 44.1; 39434 x 736 (465) 1368 53.2 and 63.7
-    // On 16 other sizes, 48 calls, the choice takes 0.6 % more than the faster of both on average, 9 % at most.  The results are the same bits either way.
+    // On 16 other sizes, 48 calls, the choice takes 0.8 % more than the faster of both on average, 9 % at most.  The results are the same bits either way.
     const int64_t steps = (c.k + Q8_BLOCK - 1) / Q8_BLOCK, end = c.residual || !c.out ? 10 : c.bias ? 7 : 4;
     const bool large = rounds(256, 256, n_cu) * (5 * end + 11 * steps) + 10 <= 5 * rounds(128, 128, n_cu) * (1 + steps);
     return large ? Q8Form{false, 256, 256} : Q8Form{false, 128, 128};
