@@ -133,7 +133,7 @@ template <int MT, int NT, int WK, int WN, bool GATE, bool WHOLE, bool CODES> __g
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 if (c.act == Q8_ACT_RELU) v[i] = v[i] < 0.f ? 0.f : v[i];
-                if constexpr (GATE) v[i] = silu(v[i]) * z[1][i];
+                if constexpr (GATE) v[i] = silu<WHOLE>(v[i]) * z[1][i];
             }
             if (c.residual) {
                 float x[4];

@@ -366,7 +366,7 @@ template <int WM, int MT, int NG, bool GATE, bool WHOLE, bool CODES, bool RES> _
                 for (int e = 0; e < 4; ++e) {
                     float &v = z[(tw * 4 + e) / P][(tw * 4 + e) % P];
                     v = TWICE ? from_sum(acc[tw][ta][e]) : acc[tw][ta][e];
-                    if constexpr (GATE) v = silu(v) * (TWICE ? from_sum(acc[4 + tw][ta][e]) : acc[4 + tw][ta][e]);
+                    if constexpr (GATE) v = silu<WHOLE>(v) * (TWICE ? from_sum(acc[4 + tw][ta][e]) : acc[4 + tw][ta][e]);
                 }
             }
             if (!GATE && c.bias) {
