@@ -17,7 +17,7 @@
  * power of two costs them no accuracy: off by 2^-4 of the value at most, from
  * 2^(e - 6) on, and by 2^(e - 10) below.  What a matrix holds stands exactly
  * in bf16 and in fp32 (beyond 2^128: as an infinity).
- * Scale bytes of a matrix that is read: 1..253 (others: the result is not defined).
+ * Scale bytes of a matrix that is read: 10..247, those that these calls write (others: the result is not defined).
  *
  * Conventions are those of aif.h: plain C, every call returns an aif_status and
  * enqueues nothing on failure (but where a HIP call fails, outputs hold anything),
@@ -52,7 +52,7 @@ typedef struct {
 } aif_q8_matrix;
 
 /* Rows of dtype: DEVICE, 16-byte aligned, row i at i * stride elements, strides multiples of 16 bytes below 2^33 elements
- * (0: rows lie close).  Widths are multiples of 16 bytes (of 8 where 8 bits come out), up to 16384. */
+ * (0: rows lie close).  Widths are multiples of 16 bytes (of 8 columns where 8 bits come out); of aif_q8_rows up to 16384. */
 typedef struct {
     aif_dtype dtype;        /* of x, residual, weight, sum_out and out                                                        */
     int32_t n_rows;
