@@ -57,3 +57,23 @@ def test_large_or_small_tiles(form, m, n, end, times):
         assert not few and (rows, cols) in ((256, 256), (128, 128))
         took = large if rows == 256 else small
         assert took <= 1.125 * min(large, small), (m, k, n, end, rows, large, small)
+
+
+def test_every_form_is_compared_with_64_bits(form):
+    """Each kernel and tile is reached, with each type and with and without a gate, by the sizes that test_gpu_q8.py and test_gpu_q8_forms.py hold against 64 bits."""
+    import test_gpu_q8 as base
+    import test_gpu_q8_forms as more
+    many = next(m.args[1] for m in base.test_linear_of_many_rows.pytestmark if m.args[0] == "m,n,k")
+    shapes = base.SHAPES + more.SHAPES + [(m, k, n) for m, n, k in many]
+    for dtype in ("f32", ""):
+        for end in ("", "bias relu residual", "gate", "gate residual"):
+            for where in ("", "codes"):
+                got = {form(m, k, n, f"{end} {where} {dtype}") for m, k, n in shapes}
+                want = {(True, 16, 128)} if where else {(True, 16, 16), (True, 32, 16), (True, 64, 16)}
+                want.add((False, 128, 128))
+                if not dtype:
+                    want.add((False, 256, 128) if "gate" in end else (False, 256, 256))
+                assert got == want, (dtype, end, where, got ^ want)
+    # blocks of 32 rows: the other file's alone
+    assert {form(*s, end) for s in more.SHAPES for end in ("", "f32", "gate", "gate residual f32")} == {(True, 32, 16)}
+    assert not any(form(*s, end)[1] == 32 for s in shapes[:len(base.SHAPES)] for end in ("", "f32"))
