@@ -10,14 +10,15 @@
 // a as well, and the next step has come, asked for a step ago.
 //
 // Blocks stay and take tile after tile: the loads run two steps ahead across a tile's end, so that the next one's codes come while this one's sums
-// are written.  With one wave to a matrix core nothing hides what else a wave issues: everything (reads of LDS, loads, the next
+// are written.  (Its stores are in the same counter as these loads and are not counted in the next tile's first two waits, which therefore see them done.)  With one wave to a matrix core nothing hides what else a wave issues: everything (reads of LDS, loads, the next
 // addresses) stands between two products, and the steps that need no branch run in a loop without one.
 //
-// The matrix cores bound large calls: 8192 x 8192 x 8192 takes 390 us, 2.8 PFLOP/s, where the instruction by itself reaches 4.1 - 4.5 on random codes
+// The matrix cores bound large calls: 8192 x 8192 x 8192 takes 389 us, 2.8 PFLOP/s, where the instruction by itself reaches 4.1 - 4.5 on random codes
 // and a library's product with one scale for all 337 us; a step of LDS reads costs little less than its products, and the clock falls to 2.1 GHz.
-// 65536 x 4096 x 4096 with residual takes 951 us: a tile's 128 KB of results take about 5 us that its products do not hide; gated 16000 x 1024 x 4096 126 us (1.39 us a
-// step, 4.6 a tile's end, most of it exponentials and reciprocals), 32000 x 512 x 2048 in 8 bits 79 us.  Tried and slower: eight waves a tile of 256 by 256 (411 us for 8192^3), two blocks a unit with tiles of 128 by 256,
-// blocks started apart in time.  fp32 (bf16 products of whole codes) 4096 x 4096 x 4096 120 us, 1.15 PFLOP/s.
+// 65536 x 4096 x 4096 takes 828 us, with residual 941: 1.4 us a step, and 6.3 or 13.4 for a tile's end, which its products do not hide (the residual: at its reading below).  Gated
+// 16000 x 1024 x 4096 122 - 128 us (1.39 us a step, 4.7 a tile's end, most of it exponentials and reciprocals), 32000 x 512 x 2048 in 8 bits 80 - 82 us.  Tried and slower: eight waves a
+// tile of 256 by 256 (411 us for 8192^3), two blocks a unit with tiles of 128 by 256, blocks started apart in time.  fp32 (bf16 products of whole codes) 4096 x 4096 x 4096 117 us, 1.17 PFLOP/s, gated
+// 206 us, gated 16000 x 1024 x 4096 243 us, 32000 x 512 x 2048 in 8 bits 161 us.
 #include "k_q8_form.h"
 #include "k_q8_product.h"
 #include "mfma_util.h"
@@ -341,7 +342,8 @@ template <int WM, int MT, int NG, bool GATE, bool WHOLE, bool CODES, bool RES> _
         auto column = [&](int i) { return n0 + wn * OWN + i * P / 16 * 64 + w_row<RUN>(i * P % 16 / 4, g * 4); };
         const int64_t row0 = m0 + wm * MT * 16 + r;
         constexpr int ESZ = WHOLE ? 4 : 2;
-        // a row's residual is read a turn before it is added
+        // A row's residual is asked for a turn before it is added.  As built that gains little: the reads stand in branches of their own, the additions in those of the
+        // stores, and the compiler has each store of a turn wait for all that is under way, the stores before it and the next tile's codes among it.
         q8_u4 res[RES ? 2 : 1][PIECES] = {};
         const char *res_at = RES ? (const char *)c.residual + (row0 * c.residual_stride + column(0)) * ESZ : nullptr;
         auto read_residual = [&](int ta) __attribute__((always_inline)) {
@@ -369,6 +371,7 @@ template <int WM, int MT, int NG, bool GATE, bool WHOLE, bool CODES, bool RES> _
                     if constexpr (GATE) v = silu<WHOLE>(v) * (TWICE ? from_sum(acc[4 + tw][ta][e]) : acc[4 + tw][ta][e]);
                 }
             }
+            // (read again for every 16 rows, and waited for together with all that is under way; kept for a tile it would take PIECES * P registers more)
             if (!GATE && c.bias) {
 #pragma unroll
                 for (int i = 0; i < PIECES; ++i) {

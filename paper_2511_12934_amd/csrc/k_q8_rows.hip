@@ -5,9 +5,11 @@
 // 32 with the last bit set where more followed (q8_odd), from which each output is rounded as from y itself: the codes are
 // those of the formula but for its last bits in 64.
 //
-// Memory bounds it: 200000 rows of 1024 in bf16 with residual, sum and codes take 289 us, 4.96 TB/s, where a copy of 1 GB reaches 5.2;
-// 32000 x 256 17.4 us, 25000 x 8192 315 us, fp32 100000 x 1024 243 us (5.46 TB/s).  A block has asked for its next rows before it works on these (as
-// many blocks as rows: 200000 x 1024 314 us, 25000 x 8192 384); a grid of 2^21 threads goes round (2^19: 300 us).  One row of 1024 takes 2.8 us.
+// Memory bounds it where rows are many: 200000 rows of 1024 in bf16 with residual, sum and codes take 289 us, 4.96 TB/s, where a copy of 1 GB reaches 5.2;
+// 25000 x 8192 315 us, fp32 100000 x 1024 243 us (5.46 TB/s).  The vector instructions, 41 a value there, take three quarters of that time beside it, at 256 and
+// 512 columns 57 a value: 32000 x 256 17.4 us, half of them instructions, 32000 x 512 30, seven tenths (two divisions and a root a lane, the weight once more for every
+// row).  A block has asked for its next rows before it works on these (as many blocks as rows: 200000 x 1024 314 us, 25000 x 8192 384) where a grid of 2^21
+// threads goes round (2^19: 300 us): not below, where each takes one turn.  One row of 1024 takes 2.8 us.
 #include "k_q8.h"
 
 #include <algorithm>
@@ -159,7 +161,9 @@ template <class T, int LPR, int V> hipError_t go(const Q8RowsCall &c, hipStream_
 
 // Lanes of a row: 64 hold 1024 columns without a barrier; where rows are too few for the device, more of them take one in less time (one row of 1024: 128
 // lanes 2.8 us, 64 3.7; 32000 rows: 65 and 58; of 4096: 512 lanes 3.7 us, 256 4.2; 50000 rows 381 and 367).  Two waves more a unit are worth the few registers they cost with 8192
-// columns of bf16 (315 us, without 406), not with fp32 (603, without 531).
+// columns of bf16 (315 us, without 406), not with fp32 (603, without 531).  Above 8192 columns 1024 threads leave 128 registers, of which fp32 wants two more (10000 x 16384
+// 409 us, 5.2 TB/s).  A width just above 1024, 2048, 4096 or 8192 leaves nearly half of the lanes without columns: 100000 x 1040 301 us (x 1024 147), 100000 x 2064 511
+// (x 2048 322), 50000 x 4112 477 (x 4096 294), 25000 x 8208 573 (x 8192 314).
 template <class T> hipError_t rows(const Q8RowsCall &c, hipStream_t s)
 {
     const int w = c.width;
@@ -173,7 +177,8 @@ template <class T> hipError_t rows(const Q8RowsCall &c, hipStream_t s)
     return go<T, 1024, 2>(c, s);
 }
 
-// A block of a matrix, BLOCK_ROWS by 128, brought into 8 bits by 256 threads: 16 of them take 128 columns of a row.
+// A block of a matrix, BLOCK_ROWS by 128, brought into 8 bits by 256 threads: 16 of them take 128 columns of a row.  A layer's 16384 x 16384 in bf16 173 us (4.65 TB/s, the
+// rows read once from memory and once more from the caches), 4096 x 4096 11.2 us, in fp32 23; by rows 200000 x 1024 in bf16 122 us (5.0 TB/s), in fp32 189 (5.4).
 template <class T, int BLOCK_ROWS> __global__ __launch_bounds__(256) void k_q8_weights(const Q8ConvertCall c)
 {
     __shared__ uint32_t tops[4];
@@ -218,7 +223,7 @@ template <class T, int BLOCK_ROWS> __global__ __launch_bounds__(256) void k_q8_w
     }
 }
 
-// Values of codes and scales: a thread takes eight columns of a row.
+// Values of codes and scales: a thread takes eight columns of a row.  200000 x 1024 to bf16 106 us (5.8 TB/s), to fp32 175.
 template <class T> __global__ __launch_bounds__(256) void k_q8_values(const Q8ConvertCall c)
 {
     const int pieces = c.width / 8;
