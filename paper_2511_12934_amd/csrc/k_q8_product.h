@@ -103,7 +103,8 @@ __device__ __forceinline__ q8_f4 mma(const Side<true> &w, const Side<true> &a, q
 // z / (1 + exp(-z)) for every z whose result is a normal number, down to -92: exp(-z) itself passes 2^128 at -88.7, and the reciprocal instruction gives
 // nothing for what is above 2^126, so that both are held 2^-8 smaller.  Off by (|z| / 2 + 6.8) 2^-23 of the result: the exponent's rounding grows with |z|, as does
 // what the last bit of z itself is worth (through the root of exp(-|z|), with the exponent's rounding made good, 7 2^-23 throughout: fp32 gated 32000 x 512 x 2048 in
-// 8 bits 181 us, with expf 192, without either 155).  The reciprocal times 2^-8 has steps of 2^-149 behind z = -81, which bf16 and codes do not see; fp32 takes half of it by z.
+// 8 bits 181 us, with expf 192, without either 155).  The reciprocal times 2^-8 has steps of 2^-149 behind z = -87, which bf16 and codes do not see; for fp32 half of the 2^-8 goes to z, and
+// it has them behind -90.
 template <bool WHOLE> __device__ __forceinline__ float silu(float z)
 {
     const float r = __builtin_amdgcn_rcpf(__builtin_amdgcn_exp2f(__builtin_fmaf(z, -1.44269504f, -8.0f)) + 0x1p-8f);
